@@ -375,6 +375,129 @@ int mcsd_commit_path(const mcsd_mask_view_t *mask, mcsd_dtype_t dtype, int32_t B
                      int32_t *out_n_ids_dev, void *hip_stream);
 
 /* ---------------------------------------------------------------------------------------------------
+ * A prefix cache in 4 bits (beyond the paper's bf16 setting): what fills it, reads it and attends over it.
+ *
+ * Format: the OCP microscaling format MXFP4.  A row (one token's key or value of one head, d channels) is d / 2 bytes of
+ * codes and d / 32 bytes of scales.  A code is E2M1 (1 sign, 2 exponent bits with bias 1, 1 fraction bit: 0, 0.5, 1, 1.5,
+ * 2, 3, 4, 6 and their negatives); the code of channel c is the low (c even) or high half of byte c / 2.  Scale byte c / 32
+ * is E8M0: the group's 32 numbers are code * 2^(byte - 127), byte 255 makes all of them NaN.  4.25 bits per number.
+ *
+ * Quantising 32 numbers whose largest magnitude is m: with f the exponent of m rounded to one fraction bit (halves up,
+ * m = 1.f * 2^f), byte = f - 2 + 127, kept within 1..254, and every code is the E2M1 number nearest to x / 2^(byte - 127),
+ * ties to the even code, beyond 6 to 6.  So no number is off by more than half a step of its binade, the largest included.
+ * A group that holds a NaN or an infinity gets byte 255 and zero codes.
+ *
+ * k_codes, k_scales, v_codes, v_scales : DEVICE uint8.  Row j of head h of sequence b starts at code byte
+ *      (seq_base[b] + h*head_stride + j*d) / 2 and scale byte (seq_base[b] + h*head_stride + j*d) / 32: offsets are in
+ *      channels, as in the other caches.  head_stride and every seq_base[b] are multiples of 128 channels, code arrays are
+ *      16-byte and scale arrays 4-byte aligned.
+ * ------------------------------------------------------------------------------------------------- */
+typedef struct mcsd_fp4_cache {
+    void *k_codes;
+    void *k_scales;
+    void *v_codes;
+    void *v_scales;
+} mcsd_fp4_cache_t;
+
+/* Tree attention over such a prefix cache: as mcsd_tree_attention_gqa with dtype MCSD_BF16 (q, k_tree, v_tree and out are
+ * bf16; d 64 or 128), except that the prefix rows are those of *cache (HOST struct).  The query rows of the query heads that
+ * share a key/value head are served together, up to 128 per workgroup, whichever heads they belong to.
+ * Precision: scores of prefix keys are exact to about 2^-13 of |q| |k| before the soft-max scale: a query, times the scale
+ * and log2 e, enters the matrix unit as three 6-bit terms per 32 channels that leave 2^-14 of the group's largest magnitude.
+ * Weights are rounded to bf16 for the product with the values (the denominator is summed in fp32); partial results of split
+ * keys are exchanged in fp32.
+ * workspace : DEVICE, mcsd_tree_attention_fp4kv_workspace(...) bytes (0: may be NULL), 256-byte aligned, prepared with
+ *             mcsd_workspace_init; the rules of mcsd_tree_attention hold.  The size for a call serves calls of the same B, H_q,
+ *             H_kv and d with fewer nodes, rows or prefix keys.
+ * Errors as mcsd_tree_attention_gqa; MCSD_EINVAL also for a cache without all four arrays (max_prefix > 0), for a misaligned
+ * one, and for a mask of another device than the current one. */
+size_t mcsd_tree_attention_fp4kv_workspace(int32_t B, int32_t H_q, int32_t H_kv, int32_t d, int32_t n_nodes,
+                                           int32_t row_begin, int32_t max_prefix);
+
+int mcsd_tree_attention_fp4kv(const mcsd_mask_view_t *mask, int32_t B, int32_t H_q, int32_t H_kv, int32_t d,
+                              int32_t row_begin, const void *q, const void *k_tree, const void *v_tree,
+                              int64_t node_stride, const mcsd_fp4_cache_t *cache, const int64_t *seq_base_dev,
+                              const int32_t *prefix_lens_dev, int64_t head_stride, int32_t max_prefix,
+                              float softmax_scale, void *out, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* Quantises rows into one layer's cache, as a prompt's keys and values come from the model:
+ *     cache row first_row[b] + t of head h  <-  k, v row t of head h of sequence b,      t = 0 .. n_rows[b] - 1
+ * dtype   : element type of k and v (MCSD_F32 or MCSD_BF16)
+ * k, v    : DEVICE; element (b, h, t, c) at b*batch_stride + h*src_head_stride + t*row_stride + c; 16-byte aligned, strides
+ *           >= 0 and multiples of 8 elements
+ * first_row_dev, n_rows_dev : DEVICE int32 [B]; n_rows is clamped to 0..max_rows; rows of the cache outside 0..capacity-1
+ *           are skipped, never touched
+ * capacity: rows every (sequence, head) of the cache can hold
+ * Limits: d 64 or 128; max_rows * H < 2^31.  max_rows == 0 does nothing.  One launch, no workspace. */
+int mcsd_store_fp4kv(mcsd_dtype_t dtype, int32_t B, int32_t H, int32_t d, int32_t max_rows, const void *k, const void *v,
+                     int64_t batch_stride, int64_t src_head_stride, int64_t row_stride, const int32_t *first_row_dev,
+                     const int32_t *n_rows_dev, const mcsd_fp4_cache_t *cache, const int64_t *seq_base_dev,
+                     int64_t head_stride, int32_t capacity, void *hip_stream);
+
+/* The reverse, for n_layers layers in one launch: the numbers that cache rows first_row[b] + t stand for (exact in bf16 but for
+ * the ends of its range) become row t of head h of sequence b of the layer's k and v.  Rows that are skipped are not written.
+ * caches : HOST array [n_layers];   k, v : HOST arrays [n_layers] of DEVICE pointers, addressed as in mcsd_store_fp4kv
+ * Limits and errors as mcsd_store_fp4kv; 1 <= n_layers <= MCSD_COMMIT_MAX_LAYERS (more: MCSD_EUNSUPPORTED). */
+int mcsd_load_fp4kv(mcsd_dtype_t dtype, int32_t B, int32_t H, int32_t d, int32_t n_layers, int32_t max_rows,
+                    const mcsd_fp4_cache_t *caches, const int64_t *seq_base_dev, int64_t head_stride, int32_t capacity,
+                    const int32_t *first_row_dev, const int32_t *n_rows_dev, void *const *k, void *const *v,
+                    int64_t batch_stride, int64_t dst_head_stride, int64_t row_stride, void *hip_stream);
+
+/* mcsd_commit_path for 4-bit caches: the accepted path's bf16 tree rows are quantised into cache rows L .. L+a-1 of every
+ * layer and head, lengths and ids are updated.  caches : HOST array [n_layers].  Arguments, clamps and errors otherwise as
+ * mcsd_commit_path with dtype MCSD_BF16; d 64 or 128.  Two launches. */
+int mcsd_commit_path_fp4kv(const mcsd_mask_view_t *mask, int32_t B, int32_t H, int32_t d, int32_t n_layers,
+                           const void *const *k_tree, const void *const *v_tree, int64_t node_stride,
+                           const mcsd_fp4_cache_t *caches, const int64_t *seq_base_dev, int64_t head_stride,
+                           int32_t max_prefix, int32_t capacity, const int32_t *out_path_dev,
+                           const int32_t *accept_len_dev, const int32_t *tokens_dev, const int32_t *new_tokens_dev,
+                           int32_t n_new, int32_t n_append, int32_t *prefix_lens_dev, int32_t *out_ids_dev,
+                           int32_t *out_n_ids_dev, void *hip_stream);
+
+/* ---------------------------------------------------------------------------------------------------
+ * Queries and keys on their way to the attention: the norm of each head's vector, then the rotation by position, then the
+ * layout [B][H][row][d] that the attention and the caches take, in one pass over the projections' output.
+ *     y = x / sqrt(mean(x^2) + eps) * weight          (no norm where the weight is NULL: y = x)
+ *     (y_a, y_b) <- (y_a cos t - y_b sin t, y_b cos t + y_a sin t),   t = position * inv_freq[i],  i = 0 .. rotary_dim/2 - 1
+ * with (a, b) = (i, i + rotary_dim/2), or (2i, 2i + 1) where interleaved; channels from rotary_dim on are not rotated.
+ * Computed in fp32 (angles in binary64, so far positions lose nothing), rounded once.  v, if given, is moved as it is.
+ *
+ * mcsd_tree_qk_norm_rope  : rows are tree nodes row_begin .. n_nodes-1, input row t being node row_begin + t; the position of
+ *                           node i of sequence b is L_b + level(i) - 1, L_b = prefix_lens[b] clamped to 0..max_prefix.  Output
+ *                           rows row_begin .. n_nodes-1 of [B][H][node_stride][d] are written, nothing else.
+ * mcsd_prompt_qk_norm_rope: rows are consecutive tokens t = 0 .. n_rows[b]-1 (n_rows clamped to 0..max_rows) at position
+ *                           first_pos[b] + t; output rows 0 .. n_rows[b]-1 of [B][H][out_row_stride][d].
+ * dtype         : element type of inputs and outputs (MCSD_F32 or MCSD_BF16); inputs and outputs must not overlap
+ * q_in, k_in, v_in : DEVICE; element (b, t, h, c) of q_in at b*q_batch_stride + t*q_row_stride + h*d + c, of k_in and v_in with
+ *                 kv_batch_stride and kv_row_stride; so they may be parts of one projection's rows.  v_in and v_out: both or
+ *                 neither (NULL).
+ * rope          : HOST struct; inv_freq DEVICE fp32 [rotary_dim/2] (radians per position), q_weight and k_weight DEVICE fp32 [d]
+ *                 or NULL, eps >= 0 and finite, rotary_dim a multiple of 16 in 0..d (0: no rotation, inv_freq not read)
+ * Limits: d 64 or 128; 16-byte aligned tensors, strides >= 0 and multiples of 8 elements; (H_q + 2 H_kv) <= 65535.
+ * One launch, no workspace.
+ * ------------------------------------------------------------------------------------------------- */
+typedef struct mcsd_rope {
+    int32_t rotary_dim;
+    int32_t interleaved;
+    float eps;
+    const float *inv_freq;
+    const float *q_weight;
+    const float *k_weight;
+} mcsd_rope_t;
+
+int mcsd_tree_qk_norm_rope(const mcsd_mask_view_t *mask, mcsd_dtype_t dtype, int32_t B, int32_t H_q, int32_t H_kv, int32_t d,
+                           int32_t row_begin, const void *q_in, const void *k_in, const void *v_in, int64_t q_batch_stride,
+                           int64_t q_row_stride, int64_t kv_batch_stride, int64_t kv_row_stride, const mcsd_rope_t *rope,
+                           const int32_t *prefix_lens_dev, int32_t max_prefix, void *q_out, void *k_out, void *v_out,
+                           int64_t node_stride, void *hip_stream);
+
+int mcsd_prompt_qk_norm_rope(mcsd_dtype_t dtype, int32_t B, int32_t H_q, int32_t H_kv, int32_t d, int32_t max_rows,
+                             const void *q_in, const void *k_in, const void *v_in, int64_t q_batch_stride,
+                             int64_t q_row_stride, int64_t kv_batch_stride, int64_t kv_row_stride, const mcsd_rope_t *rope,
+                             const int32_t *first_pos_dev, const int32_t *n_rows_dev, void *q_out, void *k_out, void *v_out,
+                             int64_t out_row_stride, void *hip_stream);
+
+/* ---------------------------------------------------------------------------------------------------
  * Early-stop decision models (Sec. 3.3; threshold beta = 0.4 in the caption of Fig. 2)
  *
  * After a draft-generation turn a small MLP predicts, for each of the W candidate sequences of each of B trees,

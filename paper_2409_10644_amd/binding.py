@@ -27,7 +27,8 @@ EXPORTS = ["mcsd_strerror", "mcsd_build_mask", "mcsd_slice_mask", "mcsd_free_mas
            "mcsd_verify_tree_workspace", "mcsd_verify_tree", "mcsd_verify_tree_sampling", "mcsd_verify_tree_tuned", "mcsd_commit_path", "mcsd_early_stop_distribution",
            "mcsd_early_stop_hidden", "mcsd_profile_next", "mcsd_stream_read", "mcsd_issue_probe", "mcsd_placement_probe", "mcsd_workspace_init",
            "mcsd_tree_attention_tuned_workspace", "mcsd_tree_attention_tuned", "mcsd_tree_attention_static",
-           "mcsd_tree_attention_plan"]
+           "mcsd_tree_attention_plan", "mcsd_tree_attention_fp4kv_workspace", "mcsd_tree_attention_fp4kv", "mcsd_store_fp4kv",
+           "mcsd_load_fp4kv", "mcsd_commit_path_fp4kv", "mcsd_tree_qk_norm_rope", "mcsd_prompt_qk_norm_rope"]
 STATIC_SCRATCH_BYTES = 24 * 1024 * 1024
 DECISION_MAX_K, MLP_MAX_LAYERS, MLP_MAX_WIDTH, MLP_MAX_INPUTS = 16, 3, 512, 8192
 
@@ -64,6 +65,17 @@ class AttentionPlan(C.Structure):
 class VerifyTuning(C.Structure):
     """mcsd_verify_tuning_t"""
     _fields_ = [("team", C.c_int32), ("polls", C.c_int32)]
+
+
+class Fp4Cache(C.Structure):
+    """mcsd_fp4_cache_t"""
+    _fields_ = [("k_codes", C.c_void_p), ("k_scales", C.c_void_p), ("v_codes", C.c_void_p), ("v_scales", C.c_void_p)]
+
+
+class Rope(C.Structure):
+    """mcsd_rope_t"""
+    _fields_ = [("rotary_dim", C.c_int32), ("interleaved", C.c_int32), ("eps", C.c_float), ("inv_freq", C.c_void_p),
+                ("q_weight", C.c_void_p), ("k_weight", C.c_void_p)]
 
 
 class McsdError(RuntimeError):
@@ -152,6 +164,26 @@ def _load() -> C.CDLL:
     lib.mcsd_tree_attention_tuned.argtypes = [C.POINTER(AttentionTuning), C.POINTER(MaskView), C.c_int, i32, C.c_float,
                                               C.c_float, i32, i32, i32, i32, i32, vp, vp, vp, i64, vp, vp, vp, vp, i64,
                                               i32, C.c_float, vp, vp, sz, vp]
+    lib.mcsd_tree_attention_fp4kv_workspace.restype = sz
+    lib.mcsd_tree_attention_fp4kv_workspace.argtypes = [i32] * 7
+    lib.mcsd_tree_attention_fp4kv.restype = C.c_int
+    lib.mcsd_tree_attention_fp4kv.argtypes = [C.POINTER(MaskView), i32, i32, i32, i32, i32, vp, vp, vp, i64, C.POINTER(Fp4Cache),
+                                              vp, vp, i64, i32, C.c_float, vp, vp, sz, vp]
+    lib.mcsd_store_fp4kv.restype = C.c_int
+    lib.mcsd_store_fp4kv.argtypes = [C.c_int, i32, i32, i32, i32, vp, vp, i64, i64, i64, vp, vp, C.POINTER(Fp4Cache), vp, i64,
+                                     i32, vp]
+    lib.mcsd_load_fp4kv.restype = C.c_int
+    lib.mcsd_load_fp4kv.argtypes = [C.c_int, i32, i32, i32, i32, i32, C.POINTER(Fp4Cache), vp, i64, i32, vp, vp, C.POINTER(vp),
+                                    C.POINTER(vp), i64, i64, i64, vp]
+    lib.mcsd_commit_path_fp4kv.restype = C.c_int
+    lib.mcsd_commit_path_fp4kv.argtypes = [C.POINTER(MaskView), i32, i32, i32, i32, C.POINTER(vp), C.POINTER(vp), i64,
+                                           C.POINTER(Fp4Cache), vp, i64, i32, i32, vp, vp, vp, vp, i32, i32, vp, vp, vp, vp]
+    lib.mcsd_tree_qk_norm_rope.restype = C.c_int
+    lib.mcsd_tree_qk_norm_rope.argtypes = [C.POINTER(MaskView), C.c_int, i32, i32, i32, i32, i32, vp, vp, vp, i64, i64, i64, i64,
+                                           C.POINTER(Rope), vp, i32, vp, vp, vp, i64, vp]
+    lib.mcsd_prompt_qk_norm_rope.restype = C.c_int
+    lib.mcsd_prompt_qk_norm_rope.argtypes = [C.c_int, i32, i32, i32, i32, i32, vp, vp, vp, i64, i64, i64, i64, C.POINTER(Rope),
+                                             vp, vp, vp, vp, vp, i64, vp]
     return lib
 
 
@@ -192,7 +224,8 @@ def _load_pycall():
 
     def setup(get_device):
         mod.setup(tuple(C.cast(getattr(lib, n), C.c_void_p).value for n in mod.names()), torch.Tensor,
-                  torch._C._cuda_getCurrentRawStream, get_device, _raise, MaskView, Mlp, C.ArgumentError)
+                  torch._C._cuda_getCurrentRawStream, get_device, _raise, MaskView, Mlp, Fp4Cache, Rope,
+                  C.ArgumentError)
 
     setup(device)
     return mod
@@ -426,6 +459,83 @@ def early_stop_distribution(mlp: Mlp, B: int, W: int, V: int, k: int, draft_rows
 def early_stop_hidden(mlp: Mlp, B: int, W: int, hidden: torch.Tensor, batch_stride: int, row_stride: int,
                       beta: float, prob: torch.Tensor, stop: torch.Tensor, stream=None) -> None:
     _pycall.early_stop_hidden(mlp, B, W, hidden, batch_stride, row_stride, beta, prob, stop, stream)
+
+
+def make_fp4_cache(k_codes: torch.Tensor, k_scales: torch.Tensor, v_codes: torch.Tensor, v_scales: torch.Tensor) -> Fp4Cache:
+    """mcsd_fp4_cache_t of one layer: uint8 tensors, codes [B][H_kv][capacity][d/2] and scales [B][H_kv][capacity][d/32] or any
+    other layout that seq_base and head_stride describe."""
+    for t in (k_codes, k_scales, v_codes, v_scales):
+        if not isinstance(t, torch.Tensor) or t.dtype != torch.uint8:
+            raise McsdError(MCSD_EINVAL, "make_fp4_cache (uint8 tensors)")
+    c = Fp4Cache(k_codes.data_ptr(), k_scales.data_ptr(), v_codes.data_ptr(), v_scales.data_ptr())
+    c._keep = (k_codes, k_scales, v_codes, v_scales)       # the struct holds raw pointers
+    return c
+
+
+def tree_attention_fp4kv_workspace(B: int, H_q: int, H_kv: int, d: int, n_nodes: int, row_begin: int, max_prefix: int) -> int:
+    return int(lib.mcsd_tree_attention_fp4kv_workspace(B, H_q, H_kv, d, n_nodes, row_begin, max_prefix))
+
+
+def tree_attention_fp4kv(view: MaskView, B: int, H_q: int, H_kv: int, d: int, row_begin: int, q: torch.Tensor,
+                         k_tree: torch.Tensor, v_tree: torch.Tensor, node_stride: int, cache: Fp4Cache,
+                         seq_base_dev: torch.Tensor, prefix_lens_dev: torch.Tensor, head_stride: int, max_prefix: int,
+                         softmax_scale: float, out: torch.Tensor, workspace: Optional[torch.Tensor], stream=None) -> None:
+    _pycall.tree_attention_fp4kv(view, B, H_q, H_kv, d, row_begin, q, k_tree, v_tree, node_stride, cache, seq_base_dev, prefix_lens_dev,
+                                 head_stride, max_prefix, softmax_scale, out, workspace, stream)
+
+
+def store_fp4kv(dtype: int, B: int, H: int, d: int, max_rows: int, k: torch.Tensor, v: torch.Tensor, batch_stride: int,
+                src_head_stride: int, row_stride: int, first_row_dev: torch.Tensor, n_rows_dev: torch.Tensor, cache: Fp4Cache,
+                seq_base_dev: torch.Tensor, head_stride: int, capacity: int, stream=None) -> None:
+    _pycall.store_fp4kv(dtype, B, H, d, max_rows, k, v, batch_stride, src_head_stride, row_stride, first_row_dev, n_rows_dev, cache,
+                        seq_base_dev, head_stride, capacity, stream)
+
+
+def load_fp4kv(dtype: int, B: int, H: int, d: int, max_rows: int, caches: Sequence[Fp4Cache], seq_base_dev: torch.Tensor,
+               head_stride: int, capacity: int, first_row_dev: torch.Tensor, n_rows_dev: torch.Tensor, k: Sequence[torch.Tensor],
+               v: Sequence[torch.Tensor], batch_stride: int, dst_head_stride: int, row_stride: int, stream=None) -> None:
+    """One call for all layers: caches / k / v are per-layer lists."""
+    _pycall.load_fp4kv(dtype, B, H, d, max_rows, caches, seq_base_dev, head_stride, capacity, first_row_dev, n_rows_dev, k, v, batch_stride,
+                       dst_head_stride, row_stride, stream)
+
+
+def commit_path_fp4kv(view: MaskView, B: int, H: int, d: int, k_tree: Sequence[torch.Tensor], v_tree: Sequence[torch.Tensor],
+                      node_stride: int, caches: Sequence[Fp4Cache], seq_base_dev: torch.Tensor, head_stride: int, max_prefix: int,
+                      capacity: int, out_path: torch.Tensor, accept_len: torch.Tensor, tokens: torch.Tensor,
+                      new_tokens: Optional[torch.Tensor], n_new: int, n_append: int, prefix_lens_dev: torch.Tensor,
+                      out_ids: torch.Tensor, out_n_ids: torch.Tensor, stream=None) -> None:
+    """One call for all layers: k_tree / v_tree / caches are per-layer lists."""
+    _pycall.commit_path_fp4kv(view, B, H, d, k_tree, v_tree, node_stride, caches, seq_base_dev, head_stride, max_prefix, capacity, out_path,
+                              accept_len, tokens, new_tokens, n_new, n_append, prefix_lens_dev, out_ids, out_n_ids, stream)
+
+
+def make_rope(rotary_dim: int, inv_freq: Optional[torch.Tensor], q_weight: Optional[torch.Tensor] = None,
+              k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6, interleaved: bool = False) -> Rope:
+    """mcsd_rope_t: inv_freq fp32 [rotary_dim/2] (at least) and norm weights fp32 [d], device tensors (None: no rotation, no norm)."""
+    for t in (inv_freq, q_weight, k_weight):
+        if t is not None and (t.dtype != torch.float32 or not t.is_contiguous()):
+            raise McsdError(MCSD_EINVAL, "make_rope (contiguous fp32 tensors)")
+    if (0 if inv_freq is None else inv_freq.numel()) * 2 < int(rotary_dim):
+        raise McsdError(MCSD_EINVAL, "make_rope (a frequency for every pair)")
+    r = Rope(int(rotary_dim), int(bool(interleaved)), float(eps), _ptr(inv_freq), _ptr(q_weight), _ptr(k_weight))
+    r._keep = (inv_freq, q_weight, k_weight)      # the struct holds raw pointers
+    return r
+
+
+def tree_qk_norm_rope(view: MaskView, dtype: int, B: int, H_q: int, H_kv: int, d: int, row_begin: int, q_in: torch.Tensor,
+                      k_in: torch.Tensor, v_in: Optional[torch.Tensor], q_batch_stride: int, q_row_stride: int, kv_batch_stride: int,
+                      kv_row_stride: int, rope: Rope, prefix_lens_dev: torch.Tensor, max_prefix: int, q_out: torch.Tensor,
+                      k_out: torch.Tensor, v_out: Optional[torch.Tensor], node_stride: int, stream=None) -> None:
+    _pycall.tree_qk_norm_rope(view, dtype, B, H_q, H_kv, d, row_begin, q_in, k_in, v_in, q_batch_stride, q_row_stride, kv_batch_stride,
+                              kv_row_stride, rope, prefix_lens_dev, max_prefix, q_out, k_out, v_out, node_stride, stream)
+
+
+def prompt_qk_norm_rope(dtype: int, B: int, H_q: int, H_kv: int, d: int, max_rows: int, q_in: torch.Tensor, k_in: torch.Tensor,
+                        v_in: Optional[torch.Tensor], q_batch_stride: int, q_row_stride: int, kv_batch_stride: int, kv_row_stride: int,
+                        rope: Rope, first_pos_dev: torch.Tensor, n_rows_dev: torch.Tensor, q_out: torch.Tensor, k_out: torch.Tensor,
+                        v_out: Optional[torch.Tensor], out_row_stride: int, stream=None) -> None:
+    _pycall.prompt_qk_norm_rope(dtype, B, H_q, H_kv, d, max_rows, q_in, k_in, v_in, q_batch_stride, q_row_stride, kv_batch_stride,
+                                kv_row_stride, rope, first_pos_dev, n_rows_dev, q_out, k_out, v_out, out_row_stride, stream)
 
 
 def stream_read(src: torch.Tensor, sink: torch.Tensor, workgroups: int = 0, stream=None) -> None:

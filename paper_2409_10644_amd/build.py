@@ -25,6 +25,9 @@ SOURCES = {
     # otherwise keeps their accumulators in the other half of the register file and copies them to and fro)
     "tree_attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
     "verify_tree.hip": ["-ffp-contract=off"],
+    "tree_attention_fp4.hip": [],
+    "fp4_cache.hip": [],
+    "qk_rope.hip": [],
     "commit_path.hip": [],
     "decision.hip": [],
     "probe.hip": [],

@@ -5,7 +5,7 @@
 // A gather-scatter of at most gamma rows per sequence and layer (H * d elements each, for K and V): one
 // workgroup per (path position, sequence, layer) moves the row of all heads with 16-byte accesses.  The lengths
 // are read by every workgroup of the copy, so they are updated by a second, tiny kernel behind it.
-#include "mcsd_internal.h"
+#include "fp4_format.h"
 
 namespace {
 
@@ -93,6 +93,56 @@ __global__ __launch_bounds__(64) void commit_finish_kernel(const CommitParams P)
     }
 }
 
+// The same into 4-bit caches: the accepted path's rows are quantised on their way (see fp4_format.h).
+struct CommitFp4Params {
+    const void *kt[MCSD_COMMIT_MAX_LAYERS];
+    const void *vt[MCSD_COMMIT_MAX_LAYERS];
+    mcsd_fp4_cache_t cache[MCSD_COMMIT_MAX_LAYERS];
+    const int64_t *seq_base;
+    const int32_t *path, *alen, *lens;
+    int64_t node_stride, head_stride;
+    int32_t H, gamma, n_nodes, max_prefix;
+    RowDiv rows;                                                           // by gamma
+};
+
+// grid (gamma * H rows / rows per workgroup, B, n_layers): row r is path position r % gamma of head r / gamma, so neighbouring
+// rows are neighbours in the cache.  Eight channels per lane: a quad holds a group and its maximum.
+template <int D>
+__global__ __launch_bounds__(256) void commit_fp4_kernel(const CommitFp4Params P)
+{
+    constexpr int LANES = D / 8, ROWS = 256 / LANES;
+    const int b = blockIdx.y, layer = blockIdx.z, c = threadIdx.x % LANES;
+    const int r = blockIdx.x * ROWS + threadIdx.x / LANES, h = row_div(r, P.rows), j = r - h * P.gamma;
+    const int acc = P.alen[b], len = P.lens[b], node = P.path[(int64_t)b * P.gamma + j];
+    const int64_t base = P.seq_base[b];
+    const char *kt = (const char *)P.kt[layer], *vt = (const char *)P.vt[layer];
+    const mcsd_fp4_cache_t cache = P.cache[layer];
+    const bool live = h < P.H && j < clamp_acc(acc, P.gamma) && node >= 0 && node < P.n_nodes;
+    uint4 k = make_uint4(0, 0, 0, 0), v = k;
+    if (live) {
+        const int64_t src = ((((int64_t)b * P.H + h) * P.node_stride + node) * D + c * 8) * 2;
+        k = *(const uint4 *)(kt + src);
+        v = *(const uint4 *)(vt + src);
+    }
+    const unsigned kw[4] = {k.x, k.y, k.z, k.w}, vw[4] = {v.x, v.y, v.z, v.w};
+    float kx[8], vx[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        kx[2 * i] = __uint_as_float(kw[i] << 16); kx[2 * i + 1] = __uint_as_float(kw[i] & 0xffff0000u);
+        vx[2 * i] = __uint_as_float(vw[i] << 16); vx[2 * i + 1] = __uint_as_float(vw[i] & 0xffff0000u);
+    }
+    unsigned kb, vb;
+    const unsigned kc = fp4_quantise8(kx, kb), vc = fp4_quantise8(vx, vb);
+    if (!live) return;
+    const int64_t at = base + h * P.head_stride + ((int64_t)clamp_len(len, P.max_prefix) + j) * D + c * 8;   // < capacity: see the copy above
+    *(unsigned *)((char *)cache.k_codes + at / 2) = kc;
+    *(unsigned *)((char *)cache.v_codes + at / 2) = vc;
+    if ((c & 3) == 0) {
+        ((unsigned char *)cache.k_scales)[at / 32] = (unsigned char)kb;
+        ((unsigned char *)cache.v_scales)[at / 32] = (unsigned char)vb;
+    }
+}
+
 }  // namespace
 
 extern "C" int mcsd_commit_path(const mcsd_mask_view_t *mask, mcsd_dtype_t dtype, int32_t B, int32_t H, int32_t d,
@@ -138,5 +188,52 @@ extern "C" int mcsd_commit_path(const mcsd_mask_view_t *mask, mcsd_dtype_t dtype
     if (e != hipSuccess) return MCSD_EHIP;
     const unsigned places = (unsigned)(mask->gamma + n_append);
     hipLaunchKernelGGL(commit_finish_kernel, dim3((places + 63) / 64, B), dim3(64), 0, st, P);
+    return mcsd_hip_status(hipGetLastError());
+}
+
+extern "C" int mcsd_commit_path_fp4kv(const mcsd_mask_view_t *mask, int32_t B, int32_t H, int32_t d, int32_t n_layers,
+                                      const void *const *k_tree, const void *const *v_tree, int64_t node_stride,
+                                      const mcsd_fp4_cache_t *caches, const int64_t *seq_base_dev, int64_t head_stride,
+                                      int32_t max_prefix, int32_t capacity, const int32_t *out_path_dev,
+                                      const int32_t *accept_len_dev, const int32_t *tokens_dev, const int32_t *new_tokens_dev,
+                                      int32_t n_new, int32_t n_append, int32_t *prefix_lens_dev, int32_t *out_ids_dev,
+                                      int32_t *out_n_ids_dev, void *hip_stream)
+{
+    if (!mask || !k_tree || !v_tree || !caches || !seq_base_dev || !out_path_dev || !accept_len_dev || !tokens_dev || !prefix_lens_dev ||
+        !out_ids_dev || !out_n_ids_dev)
+        return MCSD_EINVAL;
+    if (B < 1 || B > 65535 || H < 1 || H > 65535 || n_layers < 1) return MCSD_EINVAL;
+    if (n_layers > MCSD_COMMIT_MAX_LAYERS || (d != 64 && d != 128)) return MCSD_EUNSUPPORTED;
+    if (mask->gamma < 1 || mask->gamma > MCSD_MAX_LEVELS || mask->n_nodes < 1) return MCSD_EINVAL;
+    if (node_stride < mask->n_nodes || head_stride < 0 || max_prefix < 0) return MCSD_EINVAL;
+    if ((int64_t)max_prefix + mask->gamma > (int64_t)capacity) return MCSD_EINVAL;
+    if (n_new < 0 || n_append < 0 || n_append > n_new || (n_append > 0 && !new_tokens_dev)) return MCSD_EINVAL;
+    if (((node_stride * d) & 7) || (head_stride & 127)) return MCSD_EINVAL;
+
+    CommitFp4Params P;
+    for (int l = 0; l < MCSD_COMMIT_MAX_LAYERS; ++l) {
+        P.kt[l] = P.vt[l] = nullptr;
+        P.cache[l] = mcsd_fp4_cache_t();
+    }
+    for (int l = 0; l < n_layers; ++l) {
+        if (!k_tree[l] || !v_tree[l] || (((uintptr_t)k_tree[l] | (uintptr_t)v_tree[l]) & 15) || !fp4_cache_ok(&caches[l])) return MCSD_EINVAL;
+        P.kt[l] = k_tree[l]; P.vt[l] = v_tree[l]; P.cache[l] = caches[l];
+    }
+    P.seq_base = seq_base_dev; P.path = out_path_dev; P.alen = accept_len_dev; P.lens = prefix_lens_dev;
+    P.node_stride = node_stride; P.head_stride = head_stride;
+    P.H = H; P.gamma = mask->gamma; P.n_nodes = mask->n_nodes; P.max_prefix = max_prefix;
+    P.rows = row_div_of((uint32_t)mask->gamma);
+    hipStream_t st = (hipStream_t)hip_stream;
+    const unsigned per_wg = 256 / (d / 8);
+    auto kernel = d == 128 ? commit_fp4_kernel<128> : commit_fp4_kernel<64>;
+    mcsd_launch(MCSD_KERNEL_COMMIT_COPY, kernel, dim3(((unsigned)mask->gamma * H + per_wg - 1) / per_wg, B, n_layers), dim3(256), st, P);
+    if (hipGetLastError() != hipSuccess) return MCSD_EHIP;
+
+    CommitParams F = {};                                                   // (the second kernel looks at no cache)
+    F.path = out_path_dev; F.alen = accept_len_dev; F.tokens = tokens_dev; F.new_tokens = new_tokens_dev;
+    F.lens = prefix_lens_dev; F.ids = out_ids_dev; F.n_ids = out_n_ids_dev;
+    F.gamma = mask->gamma; F.n_nodes = mask->n_nodes; F.max_prefix = max_prefix; F.n_new = n_new; F.n_append = n_append;
+    const unsigned places = (unsigned)(mask->gamma + n_append);
+    hipLaunchKernelGGL(commit_finish_kernel, dim3((places + 63) / 64, B), dim3(64), 0, st, F);
     return mcsd_hip_status(hipGetLastError());
 }

@@ -14,15 +14,17 @@
 
 namespace {
 
-enum Fn { ATTN, ATTN_ROWS, ATTN_GQA, ATTN_FP8, ATTN_STATIC, VERIFY, VERIFY_SAMPLING, COMMIT, STOP_DIST, STOP_HIDDEN, SLICE, N_FN };
+enum Fn { ATTN, ATTN_ROWS, ATTN_GQA, ATTN_FP8, ATTN_STATIC, VERIFY, VERIFY_SAMPLING, COMMIT, STOP_DIST, STOP_HIDDEN, SLICE,
+          ATTN_FP4, STORE_FP4, LOAD_FP4, COMMIT_FP4, TREE_QK, PROMPT_QK, N_FN };
 const char *const FN_NAME[N_FN] = {"mcsd_tree_attention", "mcsd_tree_attention_rows", "mcsd_tree_attention_gqa", "mcsd_tree_attention_fp8kv",
                                    "mcsd_tree_attention_static", "mcsd_verify_tree", "mcsd_verify_tree_sampling", "mcsd_commit_path",
-                                   "mcsd_early_stop_distribution", "mcsd_early_stop_hidden", "mcsd_slice_mask"};
+                                   "mcsd_early_stop_distribution", "mcsd_early_stop_hidden", "mcsd_slice_mask", "mcsd_tree_attention_fp4kv",
+                                   "mcsd_store_fp4kv", "mcsd_load_fp4kv", "mcsd_commit_path_fp4kv", "mcsd_tree_qk_norm_rope", "mcsd_prompt_qk_norm_rope"};
 void *g_fn[N_FN];
 // torch.Tensor and its methods, torch's raw stream and device getters, and what raises on a status
 PyObject *g_tensor, *g_data_ptr, *g_numel, *g_element_size, *g_raw_stream, *g_device, *g_raise;
 // the binding's structures, and ctypes' error for an argument that is another one
-PyObject *g_mask_view, *g_mlp, *g_argument_error;
+PyObject *g_mask_view, *g_mlp, *g_fp4_cache, *g_rope, *g_argument_error;
 PyObject *g_str_data_ptr, *g_str_cuda_stream, *g_str_numel, *g_str_element_size;
 
 int64_t call_int(PyObject *method, PyObject *name, PyObject *self)
@@ -93,10 +95,9 @@ struct Args {
         return p;
     }
     // the memory of a ctypes structure of the given class, which the caller's argument keeps alive
-    void *structure(PyObject *cls)
+    void *structure(PyObject *cls) { return ok ? structure(cls, next()) : nullptr; }
+    void *structure(PyObject *cls, PyObject *o)
     {
-        if (!ok) return nullptr;
-        PyObject *o = next();
         if (!PyObject_TypeCheck(o, (PyTypeObject *)cls)) {
             PyErr_Format(g_argument_error, "argument %zd: expected %s, got %s", i, ((PyTypeObject *)cls)->tp_name, Py_TYPE(o)->tp_name);
             ok = false;
@@ -124,6 +125,20 @@ struct Args {
             } else {
                 out[k] = address(t);
             }
+        }
+        Py_DECREF(f);
+        return (int32_t)len;
+    }
+    // a sequence of 4-bit caches, one per layer
+    int32_t caches(mcsd_fp4_cache_t *out, int32_t most)
+    {
+        if (!ok) return 0;
+        PyObject *f = PySequence_Fast(next(), "expected a sequence of caches");
+        if (!f) { ok = false; return 0; }
+        const Py_ssize_t len = PySequence_Fast_GET_SIZE(f);
+        for (Py_ssize_t k = 0; ok && k < len && k < most; ++k) {
+            auto c = (const mcsd_fp4_cache_t *)structure(g_fp4_cache, PySequence_Fast_GET_ITEM(f, k));
+            if (ok) out[k] = *c;
         }
         Py_DECREF(f);
         return (int32_t)len;
@@ -297,6 +312,117 @@ PyObject *py_stop_hidden(PyObject *, PyObject *const *args, Py_ssize_t nargs)
     MCSD_UNLOCKED(mcsd_early_stop_hidden, STOP_HIDDEN, mlp, B, W, hidden, bs, rs, beta, prob, stop, st);
 }
 
+PyObject *py_attention_fp4(PyObject *, PyObject *const *args, Py_ssize_t nargs)
+{
+    Args a(args, nargs, 19);
+    auto view = (const mcsd_mask_view_t *)a.structure(g_mask_view);
+    const int32_t B = a.i32(), H = a.i32(), Hkv = a.i32(), d = a.i32(), row = a.i32();
+    void *q = a.tensor(), *kt = a.tensor(), *vt = a.tensor();
+    const int64_t node_stride = a.integer();
+    auto cache = (const mcsd_fp4_cache_t *)a.structure(g_fp4_cache);
+    auto base = (const int64_t *)a.tensor();
+    auto lens = (const int32_t *)a.tensor();
+    const int64_t head_stride = a.integer();
+    const int32_t max_prefix = a.i32();
+    const float scale = a.f32();
+    void *out = a.tensor();
+    size_t ws_bytes;
+    void *ws = a.workspace(ws_bytes);
+    void *st = a.stream();
+    MCSD_UNLOCKED(mcsd_tree_attention_fp4kv, ATTN_FP4, view, B, H, Hkv, d, row, q, kt, vt, node_stride, cache, base, lens, head_stride, max_prefix, scale, out, ws, ws_bytes, st);
+}
+
+PyObject *py_store_fp4(PyObject *, PyObject *const *args, Py_ssize_t nargs)
+{
+    Args a(args, nargs, 17);
+    const auto dtype = (mcsd_dtype_t)a.i32();
+    const int32_t B = a.i32(), H = a.i32(), d = a.i32(), rows = a.i32();
+    void *k = a.tensor(), *v = a.tensor();
+    const int64_t bs = a.integer(), hs = a.integer(), rs = a.integer();
+    auto first = (const int32_t *)a.tensor(), n = (const int32_t *)a.tensor();
+    auto cache = (const mcsd_fp4_cache_t *)a.structure(g_fp4_cache);
+    auto base = (const int64_t *)a.tensor();
+    const int64_t head_stride = a.integer();
+    const int32_t capacity = a.i32();
+    void *st = a.stream();
+    MCSD_UNLOCKED(mcsd_store_fp4kv, STORE_FP4, dtype, B, H, d, rows, k, v, bs, hs, rs, first, n, cache, base, head_stride, capacity, st);
+}
+
+PyObject *py_load_fp4(PyObject *, PyObject *const *args, Py_ssize_t nargs)
+{
+    Args a(args, nargs, 17);
+    const auto dtype = (mcsd_dtype_t)a.i32();
+    const int32_t B = a.i32(), H = a.i32(), d = a.i32(), rows = a.i32();
+    constexpr int32_t MOST = MCSD_COMMIT_MAX_LAYERS;
+    mcsd_fp4_cache_t caches[MOST];
+    const int32_t n_layers = a.caches(caches, MOST);
+    auto base = (const int64_t *)a.tensor();
+    const int64_t head_stride = a.integer();
+    const int32_t capacity = a.i32();
+    auto first = (const int32_t *)a.tensor(), n = (const int32_t *)a.tensor();
+    void *k[MOST], *v[MOST];
+    const int32_t n2 = a.tensors(k, MOST), n3 = a.tensors(v, MOST);
+    const int64_t bs = a.integer(), hs = a.integer(), rs = a.integer();
+    void *st = a.stream();
+    if (a.ok && (n2 != n_layers || n3 != n_layers)) {
+        PyErr_SetString(PyExc_AssertionError, "as many tensors per list as layers");
+        return nullptr;
+    }
+    // (more layers than the arrays hold: the entry point answers before it reads them)
+    MCSD_UNLOCKED(mcsd_load_fp4kv, LOAD_FP4, dtype, B, H, d, n_layers, rows, caches, base, head_stride, capacity, first, n, k, v, bs, hs, rs, st);
+}
+
+PyObject *py_commit_fp4(PyObject *, PyObject *const *args, Py_ssize_t nargs)
+{
+    Args a(args, nargs, 22);
+    auto view = (const mcsd_mask_view_t *)a.structure(g_mask_view);
+    const int32_t B = a.i32(), H = a.i32(), d = a.i32();
+    constexpr int32_t MOST = MCSD_COMMIT_MAX_LAYERS;
+    void *kt[MOST], *vt[MOST];
+    mcsd_fp4_cache_t caches[MOST];
+    const int32_t n_layers = a.tensors(kt, MOST), n2 = a.tensors(vt, MOST);
+    const int64_t node_stride = a.integer();
+    const int32_t n3 = a.caches(caches, MOST);
+    auto base = (const int64_t *)a.tensor();
+    const int64_t head_stride = a.integer();
+    const int32_t max_prefix = a.i32(), capacity = a.i32();
+    auto path = (const int32_t *)a.tensor(), len = (const int32_t *)a.tensor(), tokens = (const int32_t *)a.tensor(), fresh = (const int32_t *)a.tensor();
+    const int32_t n_new = a.i32(), n_append = a.i32();
+    auto lens = (int32_t *)a.tensor(), ids = (int32_t *)a.tensor(), n_ids = (int32_t *)a.tensor();
+    void *st = a.stream();
+    if (a.ok && (n2 != n_layers || n3 != n_layers)) {
+        PyErr_SetString(PyExc_AssertionError, "as many tensors per list as layers");
+        return nullptr;
+    }
+    // (more layers than the arrays hold: the entry point answers before it reads them)
+    MCSD_UNLOCKED(mcsd_commit_path_fp4kv, COMMIT_FP4, view, B, H, d, n_layers, kt, vt, node_stride, caches, base, head_stride, max_prefix, capacity, path, len, tokens, fresh,
+                  n_new, n_append, lens, ids, n_ids, st);
+}
+
+// tree_qk_norm_rope, and prompt_qk_norm_rope without a view but with a number of rows per sequence
+template <Fn FN>
+PyObject *py_qk(PyObject *, PyObject *const *args, Py_ssize_t nargs)
+{
+    Args a(args, nargs, FN == TREE_QK ? 22 : 21);
+    auto view = FN == TREE_QK ? (const mcsd_mask_view_t *)a.structure(g_mask_view) : nullptr;
+    const auto dtype = (mcsd_dtype_t)a.i32();
+    const int32_t B = a.i32(), Hq = a.i32(), Hkv = a.i32(), d = a.i32(), rows = a.i32();       // (tree: the first row)
+    void *q = a.tensor(), *k = a.tensor(), *v = a.tensor();
+    const int64_t qb = a.integer(), qr = a.integer(), kvb = a.integer(), kvr = a.integer();
+    auto rope = (const mcsd_rope_t *)a.structure(g_rope);
+    auto first = (const int32_t *)a.tensor();
+    const int32_t max_prefix = FN == TREE_QK ? a.i32() : 0;
+    auto n = FN == TREE_QK ? nullptr : (const int32_t *)a.tensor();
+    void *qo = a.tensor(), *ko = a.tensor(), *vo = a.tensor();
+    const int64_t out_row = a.integer();
+    void *st = a.stream();
+    if constexpr (FN == TREE_QK) {
+        MCSD_UNLOCKED(mcsd_tree_qk_norm_rope, FN, view, dtype, B, Hq, Hkv, d, rows, q, k, v, qb, qr, kvb, kvr, rope, first, max_prefix, qo, ko, vo, out_row, st);
+    } else {
+        MCSD_UNLOCKED(mcsd_prompt_qk_norm_rope, FN, dtype, B, Hq, Hkv, d, rows, q, k, v, qb, qr, kvb, kvr, rope, first, n, qo, ko, vo, out_row, st);
+    }
+}
+
 // slice_mask(handle, gamma, view): fills the view
 PyObject *py_slice(PyObject *, PyObject *const *args, Py_ssize_t nargs)
 {
@@ -308,18 +434,19 @@ PyObject *py_slice(PyObject *, PyObject *const *args, Py_ssize_t nargs)
     return done(((decltype(&mcsd_slice_mask))g_fn[SLICE])(mask, gamma, view), SLICE);
 }
 
-// setup(addresses of the entry points in the order of Fn, torch.Tensor, raw_stream, device, raise, MaskView, Mlp, ctypes.ArgumentError)
+// setup(addresses of the entry points in the order of Fn, torch.Tensor, raw_stream, device, raise, MaskView, Mlp, Fp4Cache, Rope,
+// ctypes.ArgumentError)
 PyObject *py_setup(PyObject *, PyObject *args)
 {
     PyObject *addr;
-    if (!PyArg_ParseTuple(args, "O!OOOOO!O!O", &PyTuple_Type, &addr, &g_tensor, &g_raw_stream, &g_device, &g_raise, &PyType_Type, &g_mask_view,
-                          &PyType_Type, &g_mlp, &g_argument_error)) return nullptr;
+    if (!PyArg_ParseTuple(args, "O!OOOOO!O!O!O!O", &PyTuple_Type, &addr, &g_tensor, &g_raw_stream, &g_device, &g_raise, &PyType_Type, &g_mask_view,
+                          &PyType_Type, &g_mlp, &PyType_Type, &g_fp4_cache, &PyType_Type, &g_rope, &g_argument_error)) return nullptr;
     if (PyTuple_GET_SIZE(addr) != N_FN) {
         PyErr_SetString(PyExc_ValueError, "one address per entry point");
         return nullptr;
     }
     for (int i = 0; i < N_FN; ++i) g_fn[i] = (void *)(uintptr_t)PyLong_AsUnsignedLongLongMask(PyTuple_GET_ITEM(addr, i));
-    for (PyObject *o : {g_tensor, g_raw_stream, g_device, g_raise, g_mask_view, g_mlp, g_argument_error}) Py_INCREF(o);       // held for the life of the process
+    for (PyObject *o : {g_tensor, g_raw_stream, g_device, g_raise, g_mask_view, g_mlp, g_fp4_cache, g_rope, g_argument_error}) Py_INCREF(o);       // held for the life of the process
     g_data_ptr = PyObject_GetAttr(g_tensor, g_str_data_ptr);
     g_numel = PyObject_GetAttr(g_tensor, g_str_numel);
     g_element_size = PyObject_GetAttr(g_tensor, g_str_element_size);
@@ -349,6 +476,12 @@ PyMethodDef METHODS[] = {
     FAST("early_stop_distribution", py_stop_distribution),
     FAST("early_stop_hidden", py_stop_hidden),
     FAST("slice_mask", py_slice),
+    FAST("tree_attention_fp4kv", py_attention_fp4),
+    FAST("store_fp4kv", py_store_fp4),
+    FAST("load_fp4kv", py_load_fp4),
+    FAST("commit_path_fp4kv", py_commit_fp4),
+    FAST("tree_qk_norm_rope", (py_qk<TREE_QK>)),
+    FAST("prompt_qk_norm_rope", (py_qk<PROMPT_QK>)),
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef MODULE = {PyModuleDef_HEAD_INIT, "_pycall", nullptr, -1, METHODS, nullptr, nullptr, nullptr, nullptr};
