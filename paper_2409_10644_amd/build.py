@@ -25,7 +25,7 @@ SOURCES = {
     # otherwise keeps their accumulators in the other half of the register file and copies them to and fro)
     "tree_attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
     "verify_tree.hip": ["-ffp-contract=off"],
-    "tree_attention_fp4.hip": [],
+    "tree_attention_fp4.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
     "fp4_cache.hip": [],
     "qk_rope.hip": [],
     "commit_path.hip": [],
