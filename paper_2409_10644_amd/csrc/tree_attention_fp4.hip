@@ -95,8 +95,8 @@ struct Cfg {
     static constexpr int KB = RW * RB;               // a wavefront's K codes in a stage; V codes and 256 bytes for scales follow
     static constexpr int WB = 2 * KB + 256, STAGE = 4 * WB;
     static constexpr int LPT = (KB >= 1024 ? 2 * KB / 1024 : 1) + 1;   // loads per wavefront and tile
-    static constexpr int VROW = 2 * D;
-    static constexpr int VBUF = OWN ? 4 * 16 * VROW : T * VROW, NV = OWN ? 1 : 2;
+    static constexpr int VROWS = OWN ? 4 * 16 : T, VCOLS = VROWS * 64;   // V in LDS: rows, bytes of 32 columns
+    static constexpr int VBUF = CB * VCOLS, NV = OWN ? 1 : 2;
     static constexpr int NS = OWN ? (D == 128 ? 3 : 4) : 5;            // stages; two workgroups per compute unit have 80 KB each
     static constexpr int RING = NS * STAGE;
     static constexpr int PP = CB * 4 / KG;           // pieces (four columns of a row per lane) that a wavefront ends up with
@@ -105,11 +105,11 @@ struct Cfg {
     static_assert(LDS <= 80 * 1024, "two workgroups per compute unit");
 };
 
-// Order of the 16-byte chunks of a V row in LDS: 16 consecutive rows written at one chunk, and what a transpose load addresses,
-// hit 16 different places of a bank row.
-template <int D>
-__device__ __forceinline__ int swz(int r) { return D == 128 ? (((r & 3) << 2) | ((r >> 2) & 3)) : ((((r >> 1) & 1) << 2) | ((r >> 2) & 3)); }
-// The same for the groups of a row of codes.
+// V in LDS: 32 columns of all rows, 64 bytes each, then the next 32 columns (so that a transpose load takes the columns as an
+// immediate offset).  Chunk c of row r stands at c ^ vswz(r): 16 consecutive rows written at one chunk hit 16 different places of a
+// bank row; a transpose load reads 8 whole rows.
+__device__ __forceinline__ int vswz(int r) { return (r >> 2) & 3; }
+// Order of the groups of a row of codes, to the same end.
 template <int D>
 __device__ __forceinline__ int swz4(int r) { return D == 128 ? (r >> 2) & 3 : (r >> 3) & 1; }
 
@@ -264,11 +264,12 @@ template <class C>
 __device__ __forceinline__ int prefix_len(const Fp4AttnParams &p, int b) { return min(max(p.lens[b], 0), p.max_prefix); }
 
 template <int D, int QBP>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void tree_attn_fp4_kernel(const Fp4AttnParams p, const int min_tiles)
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void tree_attn_fp4_kernel(const Fp4AttnParams args, const int min_tiles)
 {
+    const Fp4AttnParams &p = args;
     using C = Cfg<D, QBP>;
     __shared__ __attribute__((aligned(1024))) unsigned char lds[C::LDS];
-    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), g = lane >> 5, ln = lane & 31;
+    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
     const int qb = wave % QBP, kg = wave / QBP, w = blockIdx.x;
     const int tree_tiles = (p.n + C::T - 1) / C::T;
     auto tiles_of = [&](int len) { return tree_tiles + (int)((unsigned)(len + C::T - 1) / C::T); };
@@ -329,38 +330,38 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 
     // ---- what stays the same for all pairs ----
     const int chunk_rows = 32 * QBP, n_rows = p.n - p.row0;
-    // offsets of this lane's pieces of a tile: its own rows of codes, 16 bytes at a time, in the order that swz4 says
-    const int f_row = lane / C::GR, f_grp = (lane % C::GR) ^ swz4<D>(f_row);
-    const int f_rows_per = 64 / C::GR;                                 // rows covered by a load
-    const int sc_idx = min(lane & 31, C::RW * C::SB / 4 - 1);
-    unsigned char *const stage0 = lds + wave * C::WB;
-    unsigned char *const vbuf0 = lds + C::RING;
-    // operand addresses: K row of the lane in every block, V^T pieces
-    int k_at[C::U], k_sw[C::U], ks_at[C::U];
-#pragma unroll
-    for (int u = 0; u < C::U; ++u) {
-        const int r = (kg * C::U + u) * 32 + ln, rr = r % C::RW;
-        k_at[u] = (r / C::RW) * C::WB + rr * C::RB;
-        k_sw[u] = swz4<D>(rr);
-        ks_at[u] = (r / C::RW) * C::WB + 2 * C::KB + rr * C::SB;
-    }
-    int v_at;
-    {
-        const int j = ln & 15, grp = ln >> 4, row = (C::OWN ? wave * 16 : kg * C::U * 32) + 4 * g + (j >> 2);
-        v_at = row * C::VROW + (((grp * 2 + ((j & 3) >> 1)) ^ swz<D>(row)) * 16) + (j & 1) * 8;
-    }
-    const int d_row = lane & 15, d_unit = lane >> 4;                   // the lane's quarter row when V is converted
-
     while (left > 0) {
+        // (addresses made anew for every piece: kept over the fold they would be in memory in the loops)
+        const int lane = anew(tid) & 63, g = lane >> 5, ln = lane & 31;
+        // offsets of this lane's pieces of a tile: its own rows of codes, 16 bytes at a time, in the order that swz4 says
+        const int f_row = lane / C::GR, f_grp = (lane % C::GR) ^ swz4<D>(f_row);
+        const int f_rows_per = 64 / C::GR;                                 // rows covered by a load
+        const int sc_idx = min(lane & 31, C::RW * C::SB / 4 - 1);
+        unsigned char *const stage0 = lds + wave * C::WB;
+        // operand addresses: the lane's K row in its first block (the second is two wavefronts' rows on) and its scales, V^T pieces
+        int k_at[C::ST], ks_at, v_lo, v_hi;
+        {
+            const int r = kg * C::U * 32 + ln, rr = r % C::RW, from = (r / C::RW) * C::WB;
+#pragma unroll
+            for (int st = 0; st < C::ST; ++st) k_at[st] = from + rr * C::RB + (((2 * st + g) ^ swz4<D>(rr)) * 16);
+            ks_at = from + 2 * C::KB + rr * C::SB;
+            const int j = ln & 15, chunk = (ln >> 4) * 2 + ((j & 3) >> 1), row = (C::OWN ? wave * 16 : kg * C::U * 32) + 4 * g + (j >> 2);
+            v_lo = C::RING + row * 64 + ((chunk ^ vswz(row)) * 16) + (j & 1) * 8;
+            v_hi = C::RING + (row + 8) * 64 + ((chunk ^ vswz(row + 8)) * 16) + (j & 1) * 8;
+        }
+        constexpr int K_BLOCK = 32 / C::RW * C::WB;
+        const int d_row = lane & 15, d_unit = lane >> 4;                   // the lane's quarter row when V is converted
         // ---- a piece of one pair: tiles [tile, tile + n) of sequence b, unit ----
         const int L = uniform(prefix_len<C>(p, b)), all = tiles_of(L);
         const int n = min(left, all - tile), end = tile + n;
         const int kvh = row_div(unit, p.by_chunks), chunk = unit - kvh * p.chunks;
         const int64_t pre = p.seq_base[b] + kvh * p.head_stride, tree = ((int64_t)b * p.H_kv + kvh) * p.node_stride * D;
-        const int row = chunk * chunk_rows + qb * 32 + ln, row_c = min(row, p.rows - 1);
-        const int hq = row_div(row_c, p.by_nrows), node = p.row0 + row_c - hq * n_rows;
-        const bool mine = row < p.rows;
-        const int64_t q_row = (((int64_t)b * p.H_q + kvh * p.grp + hq) * p.node_stride + node) * D;
+        // the lane's query row: its node, and where it is in q and out
+        auto row_of = [&](int ln, int &node) __attribute__((always_inline)) {
+            const int row_c = min(chunk * chunk_rows + qb * 32 + ln, p.rows - 1), hq = row_div(row_c, p.by_nrows);
+            node = p.row0 + row_c - hq * n_rows;
+            return (((int64_t)b * p.H_q + kvh * p.grp + hq) * p.node_stride + node) * D;
+        };
         const int t0 = max(tile - tree_tiles, 0), t1 = max(end - tree_tiles, 0), n_pre = t1 - t0;     // prefix tiles
         const int n_tree = max(min(end, tree_tiles) - tile, 0);
         const unsigned char *kc = (const unsigned char *)p.cache.k_codes + pre / 2, *vc = (const unsigned char *)p.cache.v_codes + pre / 2;
@@ -388,7 +389,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
             load_to_lds4_at((g ? vsc : ksc) + sb, to + 2 * C::KB);
         };
         // 16 of this wavefront's V rows as bf16: rows `half` * 16 .. of its stage, of which `valid` exist
-        auto convert = [&](int s, int half, unsigned char *vrows, int valid) __attribute__((always_inline)) {
+        auto convert = [&](int s, int half, int vbuf, int valid) __attribute__((always_inline)) {
             const unsigned char *from = stage0 + s * C::STAGE + C::KB;
             const int r = half * 16 + d_row;
             unsigned code[D / 32];
@@ -406,16 +407,17 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
                 for (int i = 0; i < D / 32; ++i) code[i] = r < valid ? code[i] : 0u;
             }
             const float scale = fp4_scale(byte);
-            unsigned char *to = vrows + d_row * C::VROW;
+            unsigned char *to = lds + C::RING + vbuf + (wave * 16 + d_row) * 64 + (D == 128 ? d_unit : d_unit >> 1) * C::VCOLS;
 #pragma unroll
             for (int i = 0; i < D / 32; ++i)
-                *(uint4 *)(to + (((d_unit * (D / 32) + i) ^ swz<D>(d_row)) * 16)) = fp4x8_to_bf16(code[i], scale);
+                *(uint4 *)(to + (((D == 128 ? i : (d_unit & 1) * 2 + i) ^ vswz(d_row)) * 16)) = fp4x8_to_bf16(code[i], scale);
         };
-        auto read_half = [&](const unsigned char *base, int rows, bf16x8_t (&vf)[C::CB]) __attribute__((always_inline)) {
+        // V^T operands of 16 keys from row `rows` of the wavefront's on
+        auto read16 = [&](int vbuf, int rows, bf16x8_t (&vf)[C::CB]) __attribute__((always_inline)) {
 #pragma unroll
             for (int cb = 0; cb < C::CB; ++cb) {
-                const s16x4_t lo = lds_read_tr16(base + (v_at ^ ((cb * 4) * 16)) + rows * C::VROW);
-                const s16x4_t hi = lds_read_tr16(base + (v_at ^ ((cb * 4 ^ 2) * 16)) + (rows + 8) * C::VROW);
+                const s16x4_t lo = lds_read_tr16(lds + (v_lo + vbuf) + rows * 64 + cb * C::VCOLS);
+                const s16x4_t hi = lds_read_tr16(lds + (v_hi + vbuf) + rows * 64 + cb * C::VCOLS);
                 vf[cb] = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
             }
         };
@@ -434,6 +436,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
             if (x < n_pre) issue(x, x);
         // ---- the queries as terms ----
         if (n_pre > 0) {
+            int node;
+            const int64_t q_row = row_of(anew(ln), node);
 #pragma unroll
             for (int st = 0; st < C::ST; ++st) {
                 float x[32];
@@ -461,6 +465,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         // ---- the tree's own keys: bf16 operands straight from memory, values through LDS ----
         for (int t = 0; t < n_tree; ++t) {
             const int key0 = (tile + t) * C::T, lane = anew(tid) & 63, g = lane >> 5, ln = lane & 31;
+            int node;
+            const int64_t q_row = row_of(ln, node);
             const uint64_t *mrow = p.mask_bits + (int64_t)node * p.mask_words;
             f32x16_t sacc[C::U];
             uint32_t bits[C::U];
@@ -482,8 +488,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
             // values: rows beyond the tree are zeros, and so is what is no number: a weight of zero would make it NaN for rows
             // that do not see it, so those are added below where they are seen
             bool odd = false;
-            auto bring = [&](unsigned char *to, int r_tile, int r_to) {
-                constexpr int CH = C::VROW / 16;
+            auto bring = [&](int r_tile) {                             // 16 rows, to where this wavefront converts them otherwise
+                constexpr int CH = D / 8;
 #pragma unroll
                 for (int i = 0; i < CH / 4; ++i) {                     // 16 rows of CH chunks
                     const int x = i * 64 + lane, r = x / CH, ch = x % CH, key = key0 + r_tile + r;
@@ -496,18 +502,18 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
                         odd |= lo | hi;
                         wv[y] &= (lo ? 0xffff0000u : 0xffffffffu) & (hi ? 0xffffu : 0xffffffffu);
                     }
-                    *(uint4 *)(to + (r_to + r) * C::VROW + ((ch ^ swz<D>(r_to + r)) * 16)) = make_uint4(wv[0], wv[1], wv[2], wv[3]);
+                    *(uint4 *)(lds + C::RING + (ch / 4) * C::VCOLS + (wave * 16 + r) * 64 + (((ch % 4) ^ vswz(r)) * 16)) = make_uint4(wv[0], wv[1], wv[2], wv[3]);
                 }
             };
             if constexpr (C::OWN) {
                 absorb<C>(sacc, qs, g, true, bits, [&](int i, bf16x8_t (&vf)[C::CB]) {
-                    bring(vbuf0, wave * 32 + i * 16, wave * 16);
-                    read_half(vbuf0, 0, vf);
+                    bring(wave * 32 + i * 16);
+                    read16(0, 0, vf);
                 });
             } else {
-                bring(vbuf0, wave * 16, wave * 16);
+                bring(wave * 16);
                 meet();
-                absorb<C>(sacc, qs, g, true, bits, [&](int i, bf16x8_t (&vf)[C::CB]) { read_half(vbuf0, i * 16, vf); });
+                absorb<C>(sacc, qs, g, true, bits, [&](int i, bf16x8_t (&vf)[C::CB]) { read16(0, i * 16, vf); });
             }
             if (__syncthreads_or(odd)) {                               // (rare)
                 for (int u = 0; u < C::U; ++u)
@@ -531,13 +537,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         if constexpr (!C::OWN) {
             if (n_pre > 0) {
                 wait_for(min(n_pre, C::NS - 1) - 1);
-                convert(0, 0, vbuf0 + wave * 16 * C::VROW, L - t0 * C::T - wave * C::RW);
+                convert(0, 0, 0, L - t0 * C::T - wave * C::RW);
             }
         }
         int s = 0;                                                     // stage of tile x
         for (int x = 0; x < n_pre; ++x) {
             const int s1 = s + 1 == C::NS ? 0 : s + 1, s_free = s == 0 ? C::NS - 1 : s - 1;
-            unsigned char *vbuf = C::OWN ? vbuf0 : vbuf0 + (x & 1) * C::VBUF;
+            const int vbuf = C::OWN ? 0 : (x & 1) * C::VBUF;
             if constexpr (!C::OWN) meet();                             // tile x is here and converted; everyone is done with the one before
             if (C::OWN) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             if (x + C::NS - 1 < n_pre) issue(x + C::NS - 1, s_free);
@@ -548,10 +554,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
             for (int u = 0; u < C::U; ++u) {
                 u32x4_t k[C::ST];
 #pragma unroll
-                for (int st = 0; st < C::ST; ++st) k[st] = *(const u32x4_t *)(stage + k_at[u] + (((2 * st + g) ^ k_sw[u]) * 16));
+                for (int st = 0; st < C::ST; ++st) k[st] = *(const u32x4_t *)(stage + k_at[st] + u * K_BLOCK);
                 int ks;
-                if constexpr (D == 128) ks = *(const int *)(stage + ks_at[u]) >> (8 * g);
-                else ks = *(const uint16_t *)(stage + ks_at[u]) >> (8 * g);
+                if constexpr (D == 128) ks = *(const int *)(stage + ks_at + u * K_BLOCK) >> (8 * g);
+                else ks = *(const uint16_t *)(stage + ks_at + u * K_BLOCK) >> (8 * g);
                 if (u == 0) __builtin_amdgcn_s_setprio(2);
                 sacc[u] = qs.start;
 #pragma unroll
@@ -566,7 +572,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
             if constexpr (!C::OWN) {
                 if (x + 1 < n_pre) {
                     wait_for(min(n_pre - 2 - x, C::NS - 2));
-                    convert(s1, 0, vbuf0 + ((x + 1) & 1) * C::VBUF + wave * 16 * C::VROW, valid - C::T - wave * C::RW);
+                    convert(s1, 0, C::VBUF - vbuf, valid - C::T - wave * C::RW);
                 }
             }
             uint32_t bits[C::U];
@@ -577,10 +583,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
             }
             absorb<C>(sacc, qs, g, valid < C::T, bits, [&](int i, bf16x8_t (&vf)[C::CB]) __attribute__((always_inline)) {
                 if constexpr (C::OWN) {
-                    convert(s, i, vbuf0 + wave * 16 * C::VROW, valid - wave * C::RW);
-                    read_half(vbuf0, 0, vf);
+                    convert(s, i, 0, valid - wave * C::RW);
+                    read16(0, 0, vf);
                 } else {
-                    read_half(vbuf, i * 16, vf);
+                    read16(vbuf, i * 16, vf);
                 }
             });
             s = s1;
@@ -588,127 +594,131 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         __syncthreads();
 
         // ---- the wavefronts that share a block put their parts together; each ends up with PP pieces of its rows ----
-        float l_tot = half_sum(qs.l);
-        f32x4_t acc[C::PP];
-        const int lane = anew(tid) & 63, g = lane >> 5, ln = lane & 31;
-        const auto piece = [&](int x) {
-            f32x4_t v;
+        {
+            float l_tot = half_sum(qs.l);
+            f32x4_t acc[C::PP];
+            const int lane = anew(tid) & 63, g = lane >> 5, ln = lane & 31;
+            const auto piece = [&](int x) {
+                f32x4_t v;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = qs.o[x >> 2][4 * (x & 3) + e];
-            return v;
-        };
-        if constexpr (C::KG == 1) {
+                for (int e = 0; e < 4; ++e) v[e] = qs.o[x >> 2][4 * (x & 3) + e];
+                return v;
+            };
+            if constexpr (C::KG == 1) {
 #pragma unroll
-            for (int x = 0; x < C::PP; ++x) acc[x] = piece(x);
-        } else {
-            float *ml = (float *)(lds + C::XCHG);
-            auto at = [&](int o, int r, int x) { return (f32x4_t *)(lds + ((((o * (C::KG - 1) + r) * QBP + qb) * C::PP + x) * 64 + lane) * 16); };
-#pragma unroll
-            for (int o = 0; o < C::KG; ++o) {
-                if (o == kg) {
-#pragma unroll
-                    for (int x = 0; x < C::PP; ++x) acc[x] = piece(o * C::PP + x);
-                } else {
-#pragma unroll
-                    for (int x = 0; x < C::PP; ++x) *at(o, kg < o ? kg : kg - 1, x) = piece(o * C::PP + x);
-                }
-            }
-            if (g == 0) {
-                ml[(kg * QBP + qb) * 64 + ln] = qs.m_ref;
-                ml[(kg * QBP + qb) * 64 + 32 + ln] = l_tot;
-            }
-            __syncthreads();
-            float m[C::KG], M = -INFINITY;
-#pragma unroll
-            for (int k = 0; k < C::KG; ++k) {
-                m[k] = ml[(k * QBP + qb) * 64 + ln];
-                M = fmaxf(M, m[k]);
-            }
-            const float Mf = M == -INFINITY ? 0.f : M;
-            l_tot = 0.f;
-#pragma unroll
-            for (int k = 0; k < C::KG; ++k) l_tot = fmaf(ml[(k * QBP + qb) * 64 + 32 + ln], fast_exp2(m[k] - Mf), l_tot);
-            const float own = fast_exp2(qs.m_ref - Mf);
-#pragma unroll
-            for (int x = 0; x < C::PP; ++x) acc[x] *= own;
-#pragma unroll
-            for (int r = 0; r < C::KG - 1; ++r) {
-                const float wgt = fast_exp2(ml[((r < kg ? r : r + 1) * QBP + qb) * 64 + ln] - Mf);
-#pragma unroll
-                for (int x = 0; x < C::PP; ++x) acc[x] += *at(kg, r, x) * wgt;
-            }
-            qs.m_ref = M;
-        }
-        uint16_t *orow = p.out + q_row;
-        auto write_out = [&](float inv) {
-            if (!mine) return;
-#pragma unroll
-            for (int x = 0; x < C::PP; ++x) {
-                const int y = kg * C::PP + x;
-                bf16x4_t v;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = (__bf16)(acc[x][e] * inv);
-                *(bf16x4_t *)(orow + (y >> 2) * 32 + 8 * (y & 3) + 4 * g) = v;
-            }
-        };
-        if (n == all) {
-            write_out(1.f / l_tot);
-        } else {
-            // ---- one of several pieces: leave it in the workspace; whoever is last folds them in order ----
-            if (!aligned) {
-                first_piece = (int)((done - tile) / per);
-                n_pieces = (int)((done - tile + all - 1) / per) - first_piece + 1;
-            }
-            if (__hip_atomic_load(p.ws_tag, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != WS_TAG) {
-#pragma unroll
-                for (int x = 0; x < C::PP; ++x) acc[x] = (f32x4_t){NAN, NAN, NAN, NAN};
-                write_out(1.f);                                        // never prepared: its counters mean nothing
+                for (int x = 0; x < C::PP; ++x) acc[x] = piece(x);
             } else {
-                const int ln = anew(tid) & 31, g = (anew(tid) >> 5) & 1;
-                // slot of the piece: a workgroup leaves at most two, the first of them the end of a pair that began before
-                const auto slot_of = [&](int i) { return (int64_t)(2 * (first_piece + i) + (i == 0)); };
-                const int64_t slot = slot_of(w - first_piece);
-                constexpr int AGENT = 16;                              // (sc1: past this die's L2, for the other dies)
-                constexpr int ROWS = 32 * QBP;
-                if (mine) {
-                    const auto ro = __builtin_amdgcn_make_buffer_rsrc((void *)(p.part_o + slot * ROWS * D), 0, ROWS * D * 4, 0x00027000);
+                float *ml = (float *)(lds + C::XCHG);
+                auto at = [&](int o, int r, int x) { return (f32x4_t *)(lds + ((((o * (C::KG - 1) + r) * QBP + qb) * C::PP + x) * 64 + lane) * 16); };
 #pragma unroll
-                    for (int x = 0; x < C::PP; ++x)
-                        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(i32x4_t, acc[x]), ro, (((qb * C::CB * 4 + kg * C::PP + x) * 2 + g) * 32 + ln) * 16, 0, AGENT);
-                    if (kg == 0 && g == 0) {
-                        __hip_atomic_store(p.part_m + slot * ROWS + qb * 32 + ln, qs.m_ref, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                        __hip_atomic_store(p.part_l + slot * ROWS + qb * 32 + ln, l_tot, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                for (int o = 0; o < C::KG; ++o) {
+                    if (o == kg) {
+#pragma unroll
+                        for (int x = 0; x < C::PP; ++x) acc[x] = piece(o * C::PP + x);
+                    } else {
+#pragma unroll
+                        for (int x = 0; x < C::PP; ++x) *at(o, kg < o ? kg : kg - 1, x) = piece(o * C::PP + x);
                     }
                 }
-                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+                if (g == 0) {
+                    ml[(kg * QBP + qb) * 64 + ln] = qs.m_ref;
+                    ml[(kg * QBP + qb) * 64 + 32 + ln] = l_tot;
+                }
                 __syncthreads();
-                unsigned long long *const s_prev = (unsigned long long *)(lds + C::LDS - 16);
-                if (tid == 0) *s_prev = __hip_atomic_fetch_add(p.ctr + (int64_t)first_piece * CTR_STRIDE, 1ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                __syncthreads();
-                if ((int)*s_prev + 1 == n_pieces) {
-                    if (tid == 0) __hip_atomic_store(p.ctr + (int64_t)first_piece * CTR_STRIDE, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                    float M = -INFINITY;
-                    for (int i = 0; i < n_pieces; ++i)
-                        M = fmaxf(M, __hip_atomic_load(p.part_m + slot_of(i) * ROWS + qb * 32 + ln, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
-                    if (M == -INFINITY) M = 0.f;
-                    float den = 0.f;
+                float m[C::KG], M = -INFINITY;
 #pragma unroll
-                    for (int x = 0; x < C::PP; ++x) acc[x] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
-                    for (int i = 0; i < n_pieces; ++i) {
-                        const int64_t sl = slot_of(i);
-                        const float m = __hip_atomic_load(p.part_m + sl * ROWS + qb * 32 + ln, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                        const float lp = __hip_atomic_load(p.part_l + sl * ROWS + qb * 32 + ln, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                        const auto ro = __builtin_amdgcn_make_buffer_rsrc((void *)(p.part_o + sl * ROWS * D), 0, ROWS * D * 4, 0x00027000);
-                        f32x4_t v[C::PP];
+                for (int k = 0; k < C::KG; ++k) {
+                    m[k] = ml[(k * QBP + qb) * 64 + ln];
+                    M = fmaxf(M, m[k]);
+                }
+                const float Mf = M == -INFINITY ? 0.f : M;
+                l_tot = 0.f;
+#pragma unroll
+                for (int k = 0; k < C::KG; ++k) l_tot = fmaf(ml[(k * QBP + qb) * 64 + 32 + ln], fast_exp2(m[k] - Mf), l_tot);
+                const float own = fast_exp2(qs.m_ref - Mf);
+#pragma unroll
+                for (int x = 0; x < C::PP; ++x) acc[x] *= own;
+#pragma unroll
+                for (int r = 0; r < C::KG - 1; ++r) {
+                    const float wgt = fast_exp2(ml[((r < kg ? r : r + 1) * QBP + qb) * 64 + ln] - Mf);
+#pragma unroll
+                    for (int x = 0; x < C::PP; ++x) acc[x] += *at(kg, r, x) * wgt;
+                }
+                qs.m_ref = M;
+            }
+            int node;
+            uint16_t *const orow = p.out + row_of(ln, node);
+            const bool mine = chunk * chunk_rows + qb * 32 + ln < p.rows;
+            auto write_out = [&](float inv) {
+                if (!mine) return;
+#pragma unroll
+                for (int x = 0; x < C::PP; ++x) {
+                    const int y = kg * C::PP + x;
+                    bf16x4_t v;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[e] = (__bf16)(acc[x][e] * inv);
+                    *(bf16x4_t *)(orow + (y >> 2) * 32 + 8 * (y & 3) + 4 * g) = v;
+                }
+            };
+            if (n == all) {
+                write_out(1.f / l_tot);
+            } else {
+                // ---- one of several pieces: leave it in the workspace; whoever is last folds them in order ----
+                if (!aligned) {
+                    first_piece = (int)((done - tile) / per);
+                    n_pieces = (int)((done - tile + all - 1) / per) - first_piece + 1;
+                }
+                if (__hip_atomic_load(p.ws_tag, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != WS_TAG) {
+#pragma unroll
+                    for (int x = 0; x < C::PP; ++x) acc[x] = (f32x4_t){NAN, NAN, NAN, NAN};
+                    write_out(1.f);                                        // never prepared: its counters mean nothing
+                } else {
+                    const int ln = anew(tid) & 31, g = (anew(tid) >> 5) & 1;
+                    // slot of the piece: a workgroup leaves at most two, the first of them the end of a pair that began before
+                    const auto slot_of = [&](int i) { return (int64_t)(2 * (first_piece + i) + (i == 0)); };
+                    const int64_t slot = slot_of(w - first_piece);
+                    constexpr int AGENT = 16;                              // (sc1: past this die's L2, for the other dies)
+                    constexpr int ROWS = 32 * QBP;
+                    if (mine) {
+                        const auto ro = __builtin_amdgcn_make_buffer_rsrc((void *)(p.part_o + slot * ROWS * D), 0, ROWS * D * 4, 0x00027000);
 #pragma unroll
                         for (int x = 0; x < C::PP; ++x)
-                            v[x] = __builtin_bit_cast(f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(ro, (((qb * C::CB * 4 + kg * C::PP + x) * 2 + g) * 32 + ln) * 16, 0, AGENT));
-                        const float wgt = fast_exp2(m - M);
-                        den = fmaf(wgt, lp, den);
-#pragma unroll
-                        for (int x = 0; x < C::PP; ++x) acc[x] += wgt * v[x];
+                            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(i32x4_t, acc[x]), ro, (((qb * C::CB * 4 + kg * C::PP + x) * 2 + g) * 32 + ln) * 16, 0, AGENT);
+                        if (kg == 0 && g == 0) {
+                            __hip_atomic_store(p.part_m + slot * ROWS + qb * 32 + ln, qs.m_ref, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                            __hip_atomic_store(p.part_l + slot * ROWS + qb * 32 + ln, l_tot, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                        }
                     }
-                    write_out(1.f / den);
+                    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+                    __syncthreads();
+                    unsigned long long *const s_prev = (unsigned long long *)(lds + C::LDS - 16);
+                    if (tid == 0) *s_prev = __hip_atomic_fetch_add(p.ctr + (int64_t)first_piece * CTR_STRIDE, 1ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                    __syncthreads();
+                    if ((int)*s_prev + 1 == n_pieces) {
+                        if (tid == 0) __hip_atomic_store(p.ctr + (int64_t)first_piece * CTR_STRIDE, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                        float M = -INFINITY;
+                        for (int i = 0; i < n_pieces; ++i)
+                            M = fmaxf(M, __hip_atomic_load(p.part_m + slot_of(i) * ROWS + qb * 32 + ln, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+                        if (M == -INFINITY) M = 0.f;
+                        float den = 0.f;
+#pragma unroll
+                        for (int x = 0; x < C::PP; ++x) acc[x] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+                        for (int i = 0; i < n_pieces; ++i) {
+                            const int64_t sl = slot_of(i);
+                            const float m = __hip_atomic_load(p.part_m + sl * ROWS + qb * 32 + ln, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                            const float lp = __hip_atomic_load(p.part_l + sl * ROWS + qb * 32 + ln, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                            const auto ro = __builtin_amdgcn_make_buffer_rsrc((void *)(p.part_o + sl * ROWS * D), 0, ROWS * D * 4, 0x00027000);
+                            f32x4_t v[C::PP];
+#pragma unroll
+                            for (int x = 0; x < C::PP; ++x)
+                                v[x] = __builtin_bit_cast(f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(ro, (((qb * C::CB * 4 + kg * C::PP + x) * 2 + g) * 32 + ln) * 16, 0, AGENT));
+                            const float wgt = fast_exp2(m - M);
+                            den = fmaf(wgt, lp, den);
+#pragma unroll
+                            for (int x = 0; x < C::PP; ++x) acc[x] += wgt * v[x];
+                        }
+                        write_out(1.f / den);
+                    }
                 }
             }
         }
