@@ -20,6 +20,7 @@
 #include <math.h>
 
 #include <atomic>
+#include <type_traits>
 
 #include "fp4_format.h"
 
@@ -98,6 +99,7 @@ struct Cfg {
     static constexpr int VROWS = OWN ? 4 * 16 : T, VCOLS = VROWS * 64;   // V in LDS: rows, bytes of 32 columns
     static constexpr int VBUF = CB * VCOLS, NV = OWN ? 1 : 2;
     static constexpr int NS = OWN ? (D == 128 ? 3 : 4) : 5;            // stages; two workgroups per compute unit have 80 KB each
+    static constexpr int AHEAD = OWN ? NS - 1 : NS;  // tiles requested before the first is used
     static constexpr int RING = NS * STAGE;
     static constexpr int PP = CB * 4 / KG;           // pieces (four columns of a row per lane) that a wavefront ends up with
     static constexpr int XCHG = (KG - 1) * QBP * 32 * D * 4;
@@ -141,8 +143,12 @@ __device__ __forceinline__ void query_terms(const float (&x)[32], i32x6_t (&term
     for (int t = 0; t < 3; ++t) {
         const float s = __uint_as_float((unsigned)(e - 4 * t) << 23);
         term[t] = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(a, b, s);   // (elements of the two operands in turn)
+        // The instruction writes its first results while it still reads: operands that end with it may be given the result's
+        // registers (seen with the scale: wrong third terms), so they are kept alive beyond it.
+        asm volatile("" : : "v"(a), "v"(b), "v"(s), "v"(term[t]));
         if (t == 2) break;
         const f32x32_t back = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(term[t], s);
+        asm volatile("" : : "v"(term[t]), "v"(s), "v"(back));
 #pragma unroll
         for (int i = 0; i < 16; ++i) { a[i] -= back[2 * i]; b[i] -= back[2 * i + 1]; }
     }
@@ -246,22 +252,31 @@ __device__ __forceinline__ void absorb(f32x16_t (&sacc)[C::U], Block<C::D> &qs, 
     qs.l += sum;
 }
 
-// Inclusive sum over the wavefront.
-__device__ __forceinline__ int wave_scan(int v, int lane)
+// Inclusive sum and maximum over the wavefront's lanes (numbers >= 0).
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int from_lane(int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false); }
+__device__ __forceinline__ int wave_scan(int v)
 {
-#pragma unroll
-    for (int x = 1; x < 64; x <<= 1) {
-        const int o = __shfl_up(v, x);
-        if (lane >= x) v += o;
-    }
+    v += from_lane<0x111, 0xf>(v);   // from 1, 2, 4, 8 lanes below within 16, then the sums of 16 and 32
+    v += from_lane<0x112, 0xf>(v);
+    v += from_lane<0x114, 0xf>(v);
+    v += from_lane<0x118, 0xf>(v);
+    v += from_lane<0x142, 0xa>(v);
+    v += from_lane<0x143, 0xc>(v);
     return v;
+}
+__device__ __forceinline__ int wave_max(int v)
+{
+    v = max(v, from_lane<0x111, 0xf>(v));
+    v = max(v, from_lane<0x112, 0xf>(v));
+    v = max(v, from_lane<0x114, 0xf>(v));
+    v = max(v, from_lane<0x118, 0xf>(v));
+    v = max(v, from_lane<0x142, 0xa>(v));
+    v = max(v, from_lane<0x143, 0xc>(v));
+    return __builtin_amdgcn_readlane(v, 63);
 }
 __device__ __forceinline__ int wave_last(int v) { return __builtin_amdgcn_readlane(v, 63); }
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
-
-// Tiles of a sequence: the tree's, then the prefix's.
-template <class C>
-__device__ __forceinline__ int prefix_len(const Fp4AttnParams &p, int b) { return min(max(p.lens[b], 0), p.max_prefix); }
 
 template <int D, int QBP>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void tree_attn_fp4_kernel(const Fp4AttnParams args, const int min_tiles)
@@ -274,58 +289,67 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     const int tree_tiles = (p.n + C::T - 1) / C::T;
     auto tiles_of = [&](int len) { return tree_tiles + (int)((unsigned)(len + C::T - 1) / C::T); };
 
-    // ---- this workgroup's piece of the work: tiles [at, end) of the whole, or one split of one pair ----
+    // ---- this workgroup's piece of the work: `left` tiles of the whole from tile `tile` of (b, unit) on, or a split of one pair ----
+    // Lengths and bases of 64 sequences from b_lanes on, one per lane (in most calls those of all: one trip to memory).
+    int b_lanes = 0, len_l = 0;
+    int64_t base_l = 0;
+    auto fetch = [&](int b0) __attribute__((always_inline)) {
+        b_lanes = b0;
+        len_l = -1;
+        if (b0 + lane < p.B) {
+            len_l = min(max(p.lens[b0 + lane], 0), p.max_prefix);
+            base_l = p.seq_base[b0 + lane];
+        }
+    };
+    fetch(0);
     int total = 0, most = 0;                                           // tiles of one unit of every sequence
     for (int b0 = 0; b0 < p.B; b0 += 64) {
-        const int t = b0 + lane < p.B ? tiles_of(prefix_len<C>(p, b0 + lane)) : 0;
-        total += wave_last(wave_scan(t, lane));
-        int m = t;
-#pragma unroll
-        for (int x = 32; x; x >>= 1) m = max(m, __shfl_xor(m, x));
-        most = max(most, uniform(m));
+        if (b0) fetch(b0);
+        const int t = len_l >= 0 ? tiles_of(len_l) : 0;
+        total += wave_last(wave_scan(t));
+        most = max(most, wave_max(t));
     }
     int per = max((total * p.units + p.workgroups - 1) / p.workgroups, min_tiles);       // tiles of a piece
     per = max(per, (most + MAX_SPLITS - 1) / MAX_SPLITS);
     int aligned = 0;                                                   // > 0: splits of that many tiles, no piece crosses a pair
-    if (p.B * p.units <= p.workgroups && per >= most) {
-        aligned = per;
-    } else if (p.B * p.units <= p.workgroups && p.B <= 64) {
-        // the smallest size whose splits fit the grid; lanes try one each
-        const int cand = per + lane * (1 + per / 64);
-        const int len_l = lane < p.B ? tiles_of(prefix_len<C>(p, lane)) : 0;
-        int splits = 0;
-        for (int b = 0; b < p.B; ++b) splits += (__builtin_amdgcn_readlane(len_l, b) + cand - 1) / cand;
-        const unsigned long long fits = __builtin_amdgcn_ballot_w64(splits * p.units <= p.workgroups);
-        if (fits) aligned = uniform(__shfl(cand, __builtin_ctzll(fits)));
-        if (aligned > per + per / 8 + 2) aligned = 0;
+    if (p.B * p.units <= p.workgroups) {
+        if (per >= most) {
+            aligned = per;
+        } else if (p.B <= 64) {
+            // the smallest size whose splits fit the grid; lanes try one each
+            const int cand = per + lane * (1 + per / 64), t = len_l >= 0 ? tiles_of(len_l) : 0;
+            int splits = 0;
+            for (int b = 0; b < p.B; ++b) splits += (__builtin_amdgcn_readlane(t, b) + cand - 1) / cand;
+            const unsigned long long fits = __builtin_amdgcn_ballot_w64(splits * p.units <= p.workgroups);
+            if (fits) aligned = __builtin_amdgcn_readlane(cand, __builtin_ctzll(fits));
+            if (aligned > per + per / 8 + 2) aligned = 0;
+        }
     }
     if (aligned) per = aligned;
-    // the sequence and unit in which the piece begins, and the tile of theirs; first piece of the unit
-    int b = 0, unit = 0, tile = 0, n_pieces = 1, first_piece = 0, left = 0;
+    int b = -1, unit = 0, tile = 0, n_pieces = 1, first_piece = 0, left = 0;
     {
         int before = 0;
-        bool found = false;
-        for (int b0 = 0; b0 < p.B && !found; b0 += 64) {
-            const int t = b0 + lane < p.B ? tiles_of(prefix_len<C>(p, b0 + lane)) : 0;
+        const int here = aligned ? w : w * per;
+        for (int b0 = 0; b0 < p.B && b < 0; b0 += 64) {
+            if (b0 != b_lanes) fetch(b0);
+            const int t = len_l >= 0 ? tiles_of(len_l) : 0;
             const int each = aligned ? (t + per - 1) / per : t;        // per unit: splits, or tiles
-            const int upto = before + wave_scan(each * p.units, lane), here = aligned ? w : w * per;
+            const int upto = before + wave_scan(each * p.units);
             const unsigned long long mine = __builtin_amdgcn_ballot_w64(upto > here);
             if (mine) {
-                const int l = __builtin_ctzll(mine);
-                const int start = __builtin_amdgcn_readlane(upto - each * p.units, l), e = __builtin_amdgcn_readlane(each, l), t_l = __builtin_amdgcn_readlane(t, l);
+                const int l = __builtin_ctzll(mine), e = __builtin_amdgcn_readlane(each, l), t_l = __builtin_amdgcn_readlane(t, l);
+                const int after = here - (__builtin_amdgcn_readlane(upto, l) - e * p.units);
                 b = b0 + l;
-                unit = (here - start) / e;
-                const int in = here - start - unit * e;
+                unit = after / e;
+                const int in = after - unit * e;
                 tile = aligned ? in * per : in;
                 left = aligned ? min(per, t_l - tile) : per;
                 if (aligned) { n_pieces = e; first_piece = w - in; }
-                found = true;
             }
             before = wave_last(upto);
         }
-        if (!found) return;
+        if (b < 0) return;
     }
-    b = uniform(b); unit = uniform(unit); tile = uniform(tile); left = uniform(left); n_pieces = uniform(n_pieces); first_piece = uniform(first_piece);
     int64_t done = (int64_t)w * per;                                   // flat: tiles before this one
 
     // ---- what stays the same for all pairs ----
@@ -352,10 +376,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         constexpr int K_BLOCK = 32 / C::RW * C::WB;
         const int d_row = lane & 15, d_unit = lane >> 4;                   // the lane's quarter row when V is converted
         // ---- a piece of one pair: tiles [tile, tile + n) of sequence b, unit ----
-        const int L = uniform(prefix_len<C>(p, b)), all = tiles_of(L);
+        if (b >= b_lanes + 64) fetch(b);
+        const int L = __builtin_amdgcn_readlane(len_l, b - b_lanes), all = tiles_of(L);
+        const int64_t seq_at = (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)((uint64_t)base_l >> 32), b - b_lanes) << 32 |
+                                         (uint32_t)__builtin_amdgcn_readlane((int)base_l, b - b_lanes));
         const int n = min(left, all - tile), end = tile + n;
         const int kvh = row_div(unit, p.by_chunks), chunk = unit - kvh * p.chunks;
-        const int64_t pre = p.seq_base[b] + kvh * p.head_stride, tree = ((int64_t)b * p.H_kv + kvh) * p.node_stride * D;
+        const int64_t pre = seq_at + kvh * p.head_stride, tree = ((int64_t)b * p.H_kv + kvh) * p.node_stride * D;
         // the lane's query row: its node, and where it is in q and out
         auto row_of = [&](int ln, int &node) __attribute__((always_inline)) {
             const int row_c = min(chunk * chunk_rows + qb * 32 + ln, p.rows - 1), hq = row_div(row_c, p.by_nrows);
@@ -388,29 +415,37 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
             const int64_t sb = (int64_t)r0 * C::SB + min(sc_idx * 4, (last * C::SB) & ~3);
             load_to_lds4_at((g ? vsc : ksc) + sb, to + 2 * C::KB);
         };
-        // 16 of this wavefront's V rows as bf16: rows `half` * 16 .. of its stage, of which `valid` exist
-        auto convert = [&](int s, int half, int vbuf, int valid) __attribute__((always_inline)) {
+        // 16 of this wavefront's V rows, `half` * 16 .. of its stage, of which `valid` exist: the lane's quarter of one, and into
+        // the V buffer as bf16, one 16-byte chunk after the other
+        struct Codes { unsigned code[D / 32]; float scale; };
+        auto read_codes = [&](int s, int half, int valid) __attribute__((always_inline)) {
             const unsigned char *from = stage0 + s * C::STAGE + C::KB;
             const int r = half * 16 + d_row;
-            unsigned code[D / 32];
+            Codes c;
             if constexpr (D == 128) {
                 const uint4 c4 = *(const uint4 *)(from + r * C::RB + ((d_unit ^ swz4<D>(r)) * 16));
-                code[0] = c4.x; code[1] = c4.y; code[2] = c4.z; code[3] = c4.w;
+                c.code[0] = c4.x; c.code[1] = c4.y; c.code[2] = c4.z; c.code[3] = c4.w;
             } else {
                 const uint2 c2 = *(const uint2 *)(from + r * C::RB + (((d_unit >> 1) ^ swz4<D>(r)) * 16) + (d_unit & 1) * 8);
-                code[0] = c2.x; code[1] = c2.y;
+                c.code[0] = c2.x; c.code[1] = c2.y;
             }
             unsigned byte = from[C::KB + 128 + r * C::SB + (D == 128 ? d_unit : d_unit >> 1)];
             if (valid < C::RW) {                                       // (uniform) beyond the last key: zeros, whatever stands there
                 byte = r < valid ? byte : 127u;
 #pragma unroll
-                for (int i = 0; i < D / 32; ++i) code[i] = r < valid ? code[i] : 0u;
+                for (int i = 0; i < D / 32; ++i) c.code[i] = r < valid ? c.code[i] : 0u;
             }
-            const float scale = fp4_scale(byte);
-            unsigned char *to = lds + C::RING + vbuf + (wave * 16 + d_row) * 64 + (D == 128 ? d_unit : d_unit >> 1) * C::VCOLS;
+            c.scale = fp4_scale(byte);
+            return c;
+        };
+        auto write_codes = [&](const Codes &c, int i, int vbuf) __attribute__((always_inline)) {
+            *(uint4 *)(lds + C::RING + vbuf + (wave * 16 + d_row) * 64 + (D == 128 ? d_unit : d_unit >> 1) * C::VCOLS +
+                       (((D == 128 ? i : (d_unit & 1) * 2 + i) ^ vswz(d_row)) * 16)) = fp4x8_to_bf16(c.code[i], c.scale);
+        };
+        auto convert = [&](int s, int half, int vbuf, int valid) __attribute__((always_inline)) {
+            const Codes c = read_codes(s, half, valid);
 #pragma unroll
-            for (int i = 0; i < D / 32; ++i)
-                *(uint4 *)(to + (((D == 128 ? i : (d_unit & 1) * 2 + i) ^ vswz(d_row)) * 16)) = fp4x8_to_bf16(code[i], scale);
+            for (int i = 0; i < D / 32; ++i) write_codes(c, i, vbuf);
         };
         // V^T operands of 16 keys from row `rows` of the wavefront's on
         auto read16 = [&](int vbuf, int rows, bf16x8_t (&vf)[C::CB]) __attribute__((always_inline)) {
@@ -429,73 +464,79 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
             asm volatile("" ::: "memory");
         };
 
+        // The queries as they are: channels 64 st + 32 g + 8 i .. +7 (also the order of the contraction with the tree's keys).
+        uint4 qr[C::ST][4];
         __syncthreads();                                               // (LDS is free: the piece before may have folded in it)
-        Block<D> qs;
-#pragma unroll
-        for (int x = 0; x < C::NS - 1; ++x)
-            if (x < n_pre) issue(x, x);
-        // ---- the queries as terms ----
-        if (n_pre > 0) {
+        if (n_pre > 0) issue(0, 0);
+        if (n_pre > 1) issue(1, 1);
+        {
             int node;
             const int64_t q_row = row_of(anew(ln), node);
 #pragma unroll
-            for (int st = 0; st < C::ST; ++st) {
-                float x[32];
-                const uint4 *qp = (const uint4 *)(p.q + q_row + st * 64 + g * 32);
+            for (int st = 0; st < C::ST; ++st)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const uint4 v = qp[i];
-                    const unsigned wv[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-                    for (int y = 0; y < 4; ++y) {
-                        x[8 * i + 2 * y] = __uint_as_float(wv[y] << 16) * p.c;
-                        x[8 * i + 2 * y + 1] = __uint_as_float(wv[y] & 0xffff0000u) * p.c;
-                    }
-                }
-                query_terms(x, qs.term[st], qs.scale[st]);
-                __builtin_amdgcn_sched_barrier(0);
-            }
+                for (int i = 0; i < 4; ++i) qr[st][i] = ((const uint4 *)(p.q + q_row + st * 64 + g * 32))[i];
         }
+#pragma unroll
+        for (int x = 2; x < C::AHEAD; ++x)
+            if (x < n_pre) issue(x, x);
+        Block<D> qs;
 #pragma unroll
         for (int cb = 0; cb < C::CB; ++cb) qs.o[cb] = (f32x16_t){0};
         qs.start = (f32x16_t){0};
         qs.m_ref = -INFINITY;
         qs.l = 0.f;
 
-        // ---- the tree's own keys: bf16 operands straight from memory, values through LDS ----
+        // ---- the tree's own keys: bf16 operands from registers, values through LDS ----
         for (int t = 0; t < n_tree; ++t) {
             const int key0 = (tile + t) * C::T, lane = anew(tid) & 63, g = lane >> 5, ln = lane & 31;
-            int node;
-            const int64_t q_row = row_of(ln, node);
-            const uint64_t *mrow = p.mask_bits + (int64_t)node * p.mask_words;
+            // A tile of the tree's own rows: K operands, the 16 V rows that this wavefront brings (32 where they are its own), mask bits.
+            struct Tree { uint4 k[C::U][C::ST][4], v[C::OWN ? 2 : 1][D / 32]; uint64_t bits[C::U]; } tr;
+            {
+                int node;
+                row_of(ln, node);
+                const uint64_t *mrow = p.mask_bits + (int64_t)node * p.mask_words;
+#pragma unroll
+                for (int u = 0; u < C::U; ++u) {
+                    const int k0 = key0 + (kg * C::U + u) * 32;
+                    tr.bits[u] = k0 < p.n ? mrow[k0 >> 6] >> (k0 & 63) : 0;
+                    const uint16_t *kr = p.kt + tree + (int64_t)min(k0 + ln, p.n - 1) * D + g * 32;
+#pragma unroll
+                    for (int st = 0; st < C::ST; ++st)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) tr.k[u][st][i] = ((const uint4 *)(kr + st * 64))[i];
+                }
+#pragma unroll
+                for (int hf = 0; hf < (C::OWN ? 2 : 1); ++hf)
+#pragma unroll
+                    for (int i = 0; i < D / 32; ++i) {                     // 16 rows of D / 8 chunks
+                        const int x = i * 64 + lane, key = key0 + (C::OWN ? wave * 32 + hf * 16 : wave * 16) + x / (D / 8);
+                        tr.v[hf][i] = make_uint4(0, 0, 0, 0);
+                        if (key < p.n) tr.v[hf][i] = *(const uint4 *)(p.vt + tree + (int64_t)key * D + x % (D / 8) * 8);
+                    }
+            }
             f32x16_t sacc[C::U];
             uint32_t bits[C::U];
 #pragma unroll
             for (int u = 0; u < C::U; ++u) {
-                const int k0 = key0 + (kg * C::U + u) * 32;
-                bits[u] = (k0 >> 6) < p.mask_words && k0 < p.n ? (uint32_t)(mrow[k0 >> 6] >> (k0 & 63)) : 0u;
+                bits[u] = (uint32_t)tr.bits[u];
                 sacc[u] = (f32x16_t){0};
-                const uint16_t *kr = p.kt + tree + (int64_t)min(k0 + ln, p.n - 1) * D + g * 8, *qr = p.q + q_row + g * 8;
 #pragma unroll
-                for (int ks = 0; ks < D / 16; ++ks) {
-                    sacc[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const bf16x8_t *)(kr + ks * 16), *(const bf16x8_t *)(qr + ks * 16), sacc[u], 0, 0, 0);
-                    if (ks % 4 == 3) __builtin_amdgcn_sched_barrier(0);
-                }
+                for (int st = 0; st < C::ST; ++st)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        sacc[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, tr.k[u][st][i]), __builtin_bit_cast(bf16x8_t, qr[st][i]), sacc[u], 0, 0, 0);
 #pragma unroll
                 for (int r = 0; r < 16; ++r) sacc[u][r] = fmaf(sacc[u][r], p.c, qs.start[0]);
-                __builtin_amdgcn_sched_barrier(0);
             }
             // values: rows beyond the tree are zeros, and so is what is no number: a weight of zero would make it NaN for rows
             // that do not see it, so those are added below where they are seen
             bool odd = false;
-            auto bring = [&](int r_tile) {                             // 16 rows, to where this wavefront converts them otherwise
-                constexpr int CH = D / 8;
+            auto bring = [&](int hf) {
 #pragma unroll
-                for (int i = 0; i < CH / 4; ++i) {                     // 16 rows of CH chunks
-                    const int x = i * 64 + lane, r = x / CH, ch = x % CH, key = key0 + r_tile + r;
-                    uint4 v = make_uint4(0, 0, 0, 0);
-                    if (key < p.n) v = *(const uint4 *)(p.vt + tree + (int64_t)key * D + ch * 8);
-                    unsigned wv[4] = {v.x, v.y, v.z, v.w};
+                for (int i = 0; i < D / 32; ++i) {
+                    const int x = i * 64 + lane, r = x / (D / 8), ch = x % (D / 8);
+                    unsigned wv[4] = {tr.v[hf][i].x, tr.v[hf][i].y, tr.v[hf][i].z, tr.v[hf][i].w};
 #pragma unroll
                     for (int y = 0; y < 4; ++y) {
                         const bool lo = (wv[y] & 0x7f80u) == 0x7f80u, hi = (wv[y] & 0x7f800000u) == 0x7f800000u;
@@ -507,11 +548,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
             };
             if constexpr (C::OWN) {
                 absorb<C>(sacc, qs, g, true, bits, [&](int i, bf16x8_t (&vf)[C::CB]) {
-                    bring(wave * 32 + i * 16);
+                    bring(i);
                     read16(0, 0, vf);
                 });
             } else {
-                bring(wave * 16);
+                bring(0);
                 meet();
                 absorb<C>(sacc, qs, g, true, bits, [&](int i, bf16x8_t (&vf)[C::CB]) { read16(0, i * 16, vf); });
             }
@@ -533,63 +574,212 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
                     }
             }
         }
-        // ---- the prefix ----
-        if constexpr (!C::OWN) {
-            if (n_pre > 0) {
-                wait_for(min(n_pre, C::NS - 1) - 1);
-                convert(0, 0, 0, L - t0 * C::T - wave * C::RW);
+        // ---- the queries as terms ----
+        {
+#pragma unroll
+            for (int st = 0; st < C::ST; ++st) {
+                float x[32];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const unsigned wv[4] = {qr[st][i].x, qr[st][i].y, qr[st][i].z, qr[st][i].w};
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) {
+                        x[8 * i + 2 * y] = __uint_as_float(wv[y] << 16) * p.c;
+                        x[8 * i + 2 * y + 1] = __uint_as_float(wv[y] & 0xffff0000u) * p.c;
+                    }
+                }
+                query_terms(x, qs.term[st], qs.scale[st]);
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
-        int s = 0;                                                     // stage of tile x
-        for (int x = 0; x < n_pre; ++x) {
-            const int s1 = s + 1 == C::NS ? 0 : s + 1, s_free = s == 0 ? C::NS - 1 : s - 1;
-            const int vbuf = C::OWN ? 0 : (x & 1) * C::VBUF;
-            if constexpr (!C::OWN) meet();                             // tile x is here and converted; everyone is done with the one before
-            if (C::OWN) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            if (x + C::NS - 1 < n_pre) issue(x + C::NS - 1, s_free);
-            if constexpr (C::OWN) wait_for(min(n_pre - 1 - x, C::NS - 1));
-            const unsigned char *stage = lds + s * C::STAGE;
-            f32x16_t sacc[C::U];
+        // ---- the prefix ----
+        // (a register of their own from here on: what stands in the way before and after may be kept in memory, not in the loops)
 #pragma unroll
-            for (int u = 0; u < C::U; ++u) {
+        for (int st = 0; st < C::ST; ++st) {
+#pragma unroll
+            for (int t = 0; t < 3; ++t) asm volatile("" : "+v"(qs.term[st][t]));
+            asm volatile("" : "+v"(qs.scale[st]), "+v"(k_at[st]));
+        }
+        asm volatile("" : "+v"(ks_at), "+v"(v_lo), "+v"(v_hi));
+        // which keys of a tile's blocks exist
+        auto exist = [&](int valid, int u) {
+            const int here = valid - (kg * C::U + u) * 32;
+            return here >= 32 ? 0xffffffffu : here <= 0 ? 0u : (1u << here) - 1u;
+        };
+        auto read_k = [&](const unsigned char *stage, int u, u32x4_t (&k)[C::ST], int &ks) __attribute__((always_inline)) {
+#pragma unroll
+            for (int st = 0; st < C::ST; ++st) k[st] = *(const u32x4_t *)(stage + k_at[st] + u * K_BLOCK);
+            if constexpr (D == 128) ks = *(const int *)(stage + ks_at + u * K_BLOCK) >> (8 * g);
+            else ks = *(const uint16_t *)(stage + ks_at + u * K_BLOCK) >> (8 * g);
+        };
+        // step i of S^T = K Q^T: the small terms first
+        auto qk = [&](int i, f32x16_t &s, const u32x4_t (&k)[C::ST], int ks) __attribute__((always_inline)) {
+            const int st = i / 3;
+            if (i % 3 == 0) s = mfma_fp4<2>(k[st], qs.term[st][2], i == 0 ? qs.start : s, ks, qs.scale[st], st);
+            if (i % 3 == 1) s = mfma_fp4<1>(k[st], qs.term[st][1], s, ks, qs.scale[st], st);
+            if (i % 3 == 2) s = mfma_fp4<0>(k[st], qs.term[st][0], s, ks, qs.scale[st], st);
+        };
+        constexpr int NQK = 3 * C::ST, NPV = 2 * C::CB;
+        if constexpr (C::OWN) {
+            int s = 0;                                                 // stage of tile x
+            for (int x = 0; x < n_pre; ++x) {
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // (the stage of the tile before has been read)
+                if (x + C::NS - 1 < n_pre) issue(x + C::NS - 1, s == 0 ? C::NS - 1 : s - 1);
+                wait_for(min(n_pre - 1 - x, C::NS - 1));
+                f32x16_t sacc[1];
                 u32x4_t k[C::ST];
-#pragma unroll
-                for (int st = 0; st < C::ST; ++st) k[st] = *(const u32x4_t *)(stage + k_at[st] + u * K_BLOCK);
                 int ks;
-                if constexpr (D == 128) ks = *(const int *)(stage + ks_at + u * K_BLOCK) >> (8 * g);
-                else ks = *(const uint16_t *)(stage + ks_at + u * K_BLOCK) >> (8 * g);
-                if (u == 0) __builtin_amdgcn_s_setprio(2);
-                sacc[u] = qs.start;
+                read_k(lds + s * C::STAGE, 0, k, ks);
 #pragma unroll
-                for (int st = 0; st < C::ST; ++st) {
-                    sacc[u] = mfma_fp4<2>(k[st], qs.term[st][2], sacc[u], ks, qs.scale[st], st);
-                    sacc[u] = mfma_fp4<1>(k[st], qs.term[st][1], sacc[u], ks, qs.scale[st], st);
-                    sacc[u] = mfma_fp4<0>(k[st], qs.term[st][0], sacc[u], ks, qs.scale[st], st);
-                }
-            }
-            __builtin_amdgcn_s_setprio(0);
-            const int valid = L - (t0 + x) * C::T;                     // keys of this tile that exist
-            if constexpr (!C::OWN) {
-                if (x + 1 < n_pre) {
-                    wait_for(min(n_pre - 2 - x, C::NS - 2));
-                    convert(s1, 0, C::VBUF - vbuf, valid - C::T - wave * C::RW);
-                }
-            }
-            uint32_t bits[C::U];
-#pragma unroll
-            for (int u = 0; u < C::U; ++u) {
-                const int here = valid - (kg * C::U + u) * 32;
-                bits[u] = here >= 32 ? 0xffffffffu : here <= 0 ? 0u : (1u << here) - 1u;
-            }
-            absorb<C>(sacc, qs, g, valid < C::T, bits, [&](int i, bf16x8_t (&vf)[C::CB]) __attribute__((always_inline)) {
-                if constexpr (C::OWN) {
+                for (int i = 0; i < NQK; ++i) qk(i, sacc[0], k, ks);
+                const int valid = L - (t0 + x) * C::T;                 // keys of this tile that exist
+                const uint32_t bits[1] = {exist(valid, 0)};
+                absorb<C>(sacc, qs, g, valid < C::T, bits, [&](int i, bf16x8_t (&vf)[C::CB]) __attribute__((always_inline)) {
                     convert(s, i, 0, valid - wave * C::RW);
                     read16(0, 0, vf);
-                } else {
-                    read16(vbuf, i * 16, vf);
+                });
+                s = s + 1 == C::NS ? 0 : s + 1;
+            }
+        } else if (n_pre > 0) {
+            // Blocks of 32 keys in a pipeline: while the weights of block j are made, the matrix unit computes the scores of block
+            // j + 1 and adds block j - 1 to the output, instruction by instruction in turn.
+            f32x16_t S[2];
+            u32x4_t P[2][2], k[C::ST];
+            int ks = 0;
+            float alpha = 1.f;
+            bool pending = false;                                      // (uniform) the output is to be scaled by alpha once block j - 1 is in
+            // scores of the next block: its missing keys, and the reference where they outgrow it
+            auto check = [&](f32x16_t &s, int valid, int u) __attribute__((always_inline)) {
+                if (valid < C::T) {
+                    const uint32_t own = exist(valid, u) >> (4 * g);
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const uint32_t seen = (uint32_t)__builtin_amdgcn_sbfe((int)own, 8 * (r / 4) + r % 4, 1);
+                        s[r] = __uint_as_float((__float_as_uint(s[r]) & seen) | (0xff800000u & ~seen));
+                    }
                 }
-            });
-            s = s1;
+                float mx = fmaxf(s[0], s[1]);
+#pragma unroll
+                for (int r = 2; r < 16; r += 2) mx = fmaxf(fmaxf(mx, s[r]), s[r + 1]);
+                mx = half_max(mx);
+                const bool none = qs.m_ref == -INFINITY, grow = none ? mx > -INFINITY : mx > SLACK;
+                if (__builtin_amdgcn_ballot_w64(grow) != 0) {
+                    const float by = grow ? mx : 0.f;
+                    alpha = none ? 0.f : fast_exp2(-by);
+                    pending = true;
+                    if (grow) qs.m_ref = (none ? 0.f : qs.m_ref) + mx;
+                    qs.l *= alpha;
+                    const float start = qs.m_ref == -INFINITY ? 0.f : -qs.m_ref;
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) qs.start[r] = start;
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) s[r] -= by;
+                }
+            };
+            // weights of `cur` into pn; scores of the next block into nxt; pp times 32 rows of V from `vrow` on into the output;
+            // CONV: this wavefront's share of a tile's V converted on the way.  Beside the last block the scores are of whatever K
+            // the registers hold, unused; before the first one pp and the V rows are zeros.
+            auto slot = [&](auto conv, f32x16_t &cur, f32x16_t &nxt, const u32x4_t (&pp)[2], u32x4_t (&pn)[2], int vbuf, int vrow, int cs, int cbuf,
+                            int cvalid) __attribute__((always_inline)) {
+                constexpr bool CONV = decltype(conv)::value;
+                bf16x8_t vf[2][C::CB];
+                read16(vbuf, vrow, vf[0]);
+                Codes cv;
+                if (CONV) cv = read_codes(cs, 0, cvalid);
+                __builtin_amdgcn_sched_barrier(0);
+                float sum = 0.f;
+#pragma unroll
+                for (int i = 0; i < NQK + NPV; ++i) {
+                    if (i < NQK) qk(i, nxt, k, ks);
+                    else {
+                        const int y = i - NQK;
+                        qs.o[y % C::CB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[y / C::CB][y % C::CB], __builtin_bit_cast(bf16x8_t, pp[y / C::CB]), qs.o[y % C::CB], 0, 0, 0);
+                    }
+#pragma unroll
+                    for (int x = 0; x < 8; ++x)                        // vector work beside it
+                        if ((D == 128 ? x : x < 6 ? x / 2 : x - 3) == i) weigh2(cur, 2 * x, sum, pn);
+                    if (CONV) {
+#pragma unroll
+                        for (int x = 0; x < D / 32; ++x)
+                            if ((D == 128 ? 8 : 5) + x == i) write_codes(cv, x, cbuf);
+                    }
+                    if (i == NQK - 1) read16(vbuf, vrow + 16, vf[1]);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                qs.l += sum;
+                if (pending) {
+                    pending = false;
+#pragma unroll
+                    for (int cb = 0; cb < C::CB; ++cb)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) qs.o[cb][r] *= alpha;
+                }
+            };
+            auto last_pv = [&](const u32x4_t (&pp)[2], int vbuf, int vrow) __attribute__((always_inline)) {
+#pragma unroll
+                for (int hf = 0; hf < 2; ++hf) {
+                    bf16x8_t vf[C::CB];
+                    read16(vbuf, vrow + hf * 16, vf);
+#pragma unroll
+                    for (int cb = 0; cb < C::CB; ++cb)
+                        qs.o[cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[cb], __builtin_bit_cast(bf16x8_t, pp[hf]), qs.o[cb], 0, 0, 0);
+                }
+            };
+            constexpr std::true_type YES;
+            constexpr std::false_type NO;
+            const int valid0 = L - t0 * C::T;                          // keys of the first tile on
+            auto next = [](int s) { return s + 1 == C::NS ? 0 : s + 1; };
+            // a tile's own slot is over: its V is converted everywhere, its stage free, and tile `need` has arrived everywhere
+            auto turn = [&](int x, int s, int need) __attribute__((always_inline)) {
+                if (need < n_pre) wait_for(min(n_pre - 1, x + C::NS - 1) - need);
+                meet();
+                if (x + C::NS < n_pre) issue(x + C::NS, s);
+            };
+#pragma unroll
+            for (int i = 0; i < C::VBUF / 4096; ++i) *(uint4 *)(lds + C::RING + C::VBUF + i * 4096 + anew(tid) * 16) = make_uint4(0, 0, 0, 0);
+            P[1][0] = P[1][1] = (u32x4_t){0, 0, 0, 0};
+            wait_for(min(n_pre, C::AHEAD) - 1 - (C::U == 1 && n_pre > 1));
+            meet();
+            read_k(lds, 0, k, ks);
+#pragma unroll
+            for (int i = 0; i < NQK; ++i) qk(i, S[0], k, ks);
+            int s = 0, x = 0;                                          // stage of tile x
+            if constexpr (C::U == 2) {
+                read_k(lds, 1, k, ks);
+                check(S[0], valid0, 0);
+                while (true) {
+                    const int vb = (x & 1) * C::VBUF, s1 = next(s), valid = valid0 - x * C::T;
+                    slot(YES, S[0], S[1], P[1], P[0], C::VBUF - vb, 32, s, vb, valid - wave * C::RW);
+                    turn(x, s, x + 1);
+                    read_k(lds + s1 * C::STAGE, 0, k, ks);
+                    check(S[1], valid, 1);
+                    slot(NO, S[1], S[0], P[0], P[1], vb, 0, 0, 0, 0);
+                    read_k(lds + s1 * C::STAGE, 1, k, ks);
+                    s = s1;
+                    if (++x == n_pre) break;
+                    check(S[0], valid - C::T, 0);
+                }
+                last_pv(P[1], ((n_pre - 1) & 1) * C::VBUF, 32);
+            } else {
+                read_k(lds + C::STAGE, 0, k, ks);
+                check(S[0], valid0, 0);
+                auto one = [&](f32x16_t &cur, f32x16_t &nxt, const u32x4_t (&pp)[2], u32x4_t (&pn)[2], int vb) __attribute__((always_inline)) {
+                    const int s1 = next(s), valid = valid0 - x * C::T;
+                    slot(YES, cur, nxt, pp, pn, C::VBUF - vb, 0, s, vb, valid - wave * C::RW);
+                    turn(x, s, x + 2);
+                    read_k(lds + next(s1) * C::STAGE, 0, k, ks);
+                    s = s1;
+                    if (++x == n_pre) return true;
+                    check(nxt, valid - C::T, 0);
+                    return false;
+                };
+                while (true) {
+                    if (one(S[0], S[1], P[1], P[0], 0)) break;
+                    if (one(S[1], S[0], P[0], P[1], C::VBUF)) break;
+                }
+                if (n_pre & 1) last_pv(P[0], 0, 0);
+                else last_pv(P[1], C::VBUF, 0);
+            }
         }
         __syncthreads();
 
@@ -696,26 +886,42 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
                     __syncthreads();
                     if ((int)*s_prev + 1 == n_pieces) {
                         if (tid == 0) __hip_atomic_store(p.ctr + (int64_t)first_piece * CTR_STRIDE, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                        float M = -INFINITY;
-                        for (int i = 0; i < n_pieces; ++i)
-                            M = fmaxf(M, __hip_atomic_load(p.part_m + slot_of(i) * ROWS + qb * 32 + ln, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
-                        if (M == -INFINITY) M = 0.f;
-                        float den = 0.f;
+                        // NF pieces at a time, everything of them requested at once; beyond the last one loads give zero
+                        constexpr int NF = C::PP >= 16 ? 2 : C::PP == 8 ? 4 : 8;
+                        const auto off_of = [&](int i) { return (2 * i + (i == 0)) * ROWS; };
+                        const auto rm = __builtin_amdgcn_make_buffer_rsrc((void *)(p.part_m + (int64_t)2 * first_piece * ROWS), 0, 2 * n_pieces * ROWS * 4, 0x00027000);
+                        const auto rl = __builtin_amdgcn_make_buffer_rsrc((void *)(p.part_l + (int64_t)2 * first_piece * ROWS), 0, 2 * n_pieces * ROWS * 4, 0x00027000);
+                        const auto ro = __builtin_amdgcn_make_buffer_rsrc((void *)(p.part_o + (int64_t)2 * first_piece * ROWS * D), 0, 2 * n_pieces * ROWS * D * 4, 0x00027000);
+                        float M = -INFINITY, den = 0.f;
 #pragma unroll
                         for (int x = 0; x < C::PP; ++x) acc[x] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
-                        for (int i = 0; i < n_pieces; ++i) {
-                            const int64_t sl = slot_of(i);
-                            const float m = __hip_atomic_load(p.part_m + sl * ROWS + qb * 32 + ln, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                            const float lp = __hip_atomic_load(p.part_l + sl * ROWS + qb * 32 + ln, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                            const auto ro = __builtin_amdgcn_make_buffer_rsrc((void *)(p.part_o + sl * ROWS * D), 0, ROWS * D * 4, 0x00027000);
-                            f32x4_t v[C::PP];
+                        for (int i0 = 0; i0 < n_pieces; i0 += NF) {
+                            float m[NF], lp[NF];
+                            f32x4_t v[NF][C::PP];
 #pragma unroll
-                            for (int x = 0; x < C::PP; ++x)
-                                v[x] = __builtin_bit_cast(f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(ro, (((qb * C::CB * 4 + kg * C::PP + x) * 2 + g) * 32 + ln) * 16, 0, AGENT));
-                            const float wgt = fast_exp2(m - M);
-                            den = fmaf(wgt, lp, den);
+                            for (int i = 0; i < NF; ++i) {
+                                m[i] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rm, (off_of(i0 + i) + qb * 32 + ln) * 4, 0, AGENT));
+                                lp[i] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rl, (off_of(i0 + i) + qb * 32 + ln) * 4, 0, AGENT));
 #pragma unroll
-                            for (int x = 0; x < C::PP; ++x) acc[x] += wgt * v[x];
+                                for (int x = 0; x < C::PP; ++x)
+                                    v[i][x] = __builtin_bit_cast(f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(ro, off_of(i0 + i) * D * 4 + (((qb * C::CB * 4 + kg * C::PP + x) * 2 + g) * 32 + ln) * 16, 0, AGENT));
+                            }
+                            __builtin_amdgcn_sched_barrier(0);
+                            float Mn = M;
+#pragma unroll
+                            for (int i = 0; i < NF; ++i) Mn = fmaxf(Mn, i0 + i < n_pieces ? m[i] : -INFINITY);
+                            const float Mf = Mn == -INFINITY ? 0.f : Mn, a = fast_exp2(M - Mf);
+                            M = Mn;
+                            den *= a;
+#pragma unroll
+                            for (int x = 0; x < C::PP; ++x) acc[x] *= a;
+#pragma unroll
+                            for (int i = 0; i < NF; ++i) {
+                                const float wgt = i0 + i < n_pieces ? fast_exp2(m[i] - Mf) : 0.f;
+                                den = fmaf(wgt, lp[i], den);
+#pragma unroll
+                                for (int x = 0; x < C::PP; ++x) acc[x] += wgt * v[i][x];
+                            }
                         }
                         write_out(1.f / den);
                     }
