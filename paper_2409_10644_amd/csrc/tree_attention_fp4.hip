@@ -98,7 +98,7 @@ struct Cfg {
     static constexpr int LPT = (KB >= 1024 ? 2 * KB / 1024 : 1) + 1;   // loads per wavefront and tile
     static constexpr int VROWS = OWN ? 4 * 16 : T, VCOLS = VROWS * 64;   // V in LDS: rows, bytes of 32 columns
     static constexpr int VBUF = CB * VCOLS, NV = OWN ? 1 : 2;
-    static constexpr int NS = OWN ? (D == 128 ? 3 : 4) : 5;            // stages; two workgroups per compute unit have 80 KB each
+    static constexpr int NS = OWN ? (D == 128 ? 3 : 4) : 4;            // stages; two workgroups per compute unit have 80 KB each
     static constexpr int AHEAD = OWN ? NS - 1 : NS;  // tiles requested before the first is used
     static constexpr int RING = NS * STAGE;
     static constexpr int PP = CB * 4 / KG;           // pieces (four columns of a row per lane) that a wavefront ends up with
@@ -170,13 +170,13 @@ __device__ __forceinline__ int anew(int v)
     return v;
 }
 
-// Weights of a pair of scores, added to the sum and packed.
+// Weights of a pair of scores, packed, and their sum as they are packed (so that numerator and denominator agree).
 __device__ __forceinline__ void weigh2(const f32x16_t &s, int r, float &sum, u32x4_t *pb)
 {
-    const float p0 = fast_exp2(s[r]), p1 = fast_exp2(s[r + 1]);
-    sum += p0 + p1;
-    unsigned u = __builtin_bit_cast(unsigned, (bf16x2_t){(__bf16)p0, (__bf16)p1});
+    const bf16x2_t one = {(__bf16)1.f, (__bf16)1.f};
+    unsigned u = __builtin_bit_cast(unsigned, (bf16x2_t){(__bf16)fast_exp2(s[r]), (__bf16)fast_exp2(s[r + 1])});
     asm volatile("" : "+v"(u));      // (stays where it is written, between two matrix instructions)
+    sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, u), one, sum, false);
     pb[r / 8][(r % 8) / 2] = u;
 }
 
@@ -417,7 +417,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         };
         // 16 of this wavefront's V rows, `half` * 16 .. of its stage, of which `valid` exist: the lane's quarter of one, and into
         // the V buffer as bf16, one 16-byte chunk after the other
-        struct Codes { unsigned code[D / 32]; float scale; };
+        struct Codes { unsigned code[D / 32], byte; };
         auto read_codes = [&](int s, int half, int valid) __attribute__((always_inline)) {
             const unsigned char *from = stage0 + s * C::STAGE + C::KB;
             const int r = half * 16 + d_row;
@@ -435,12 +435,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 #pragma unroll
                 for (int i = 0; i < D / 32; ++i) c.code[i] = r < valid ? c.code[i] : 0u;
             }
-            c.scale = fp4_scale(byte);
+            c.byte = byte;
             return c;
         };
         auto write_codes = [&](const Codes &c, int i, int vbuf) __attribute__((always_inline)) {
             *(uint4 *)(lds + C::RING + vbuf + (wave * 16 + d_row) * 64 + (D == 128 ? d_unit : d_unit >> 1) * C::VCOLS +
-                       (((D == 128 ? i : (d_unit & 1) * 2 + i) ^ vswz(d_row)) * 16)) = fp4x8_to_bf16(c.code[i], c.scale);
+                       (((D == 128 ? i : (d_unit & 1) * 2 + i) ^ vswz(d_row)) * 16)) = fp4x8_to_bf16(c.code[i], fp4_scale(c.byte));
         };
         auto convert = [&](int s, int half, int vbuf, int valid) __attribute__((always_inline)) {
             const Codes c = read_codes(s, half, valid);
@@ -648,6 +648,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
             int ks = 0;
             float alpha = 1.f;
             bool pending = false;                                      // (uniform) the output is to be scaled by alpha once block j - 1 is in
+            float limit = qs.m_ref == -INFINITY ? -INFINITY : SLACK;   // what a score may be before the reference moves (none seen yet: any does)
             // scores of the next block: its missing keys, and the reference where they outgrow it
             auto check = [&](f32x16_t &s, int valid, int u) __attribute__((always_inline)) {
                 if (valid < C::T) {
@@ -661,13 +662,17 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
                 float mx = fmaxf(s[0], s[1]);
 #pragma unroll
                 for (int r = 2; r < 16; r += 2) mx = fmaxf(fmaxf(mx, s[r]), s[r + 1]);
-                mx = half_max(mx);
-                const bool none = qs.m_ref == -INFINITY, grow = none ? mx > -INFINITY : mx > SLACK;
-                if (__builtin_amdgcn_ballot_w64(grow) != 0) {
+                // (the other half's keys are looked at when any lane's ask for it)
+                if (__builtin_expect(__builtin_amdgcn_ballot_w64(mx > limit) != 0, 0)) {
+                    mx = half_max(mx);
+                    const bool none = qs.m_ref == -INFINITY, grow = mx > limit;
                     const float by = grow ? mx : 0.f;
-                    alpha = none ? 0.f : fast_exp2(-by);
+                    alpha = grow && none ? 0.f : fast_exp2(-by);
                     pending = true;
-                    if (grow) qs.m_ref = (none ? 0.f : qs.m_ref) + mx;
+                    if (grow) {
+                        qs.m_ref = (none ? 0.f : qs.m_ref) + mx;
+                        limit = SLACK;
+                    }
                     qs.l *= alpha;
                     const float start = qs.m_ref == -INFINITY ? 0.f : -qs.m_ref;
 #pragma unroll
@@ -706,6 +711,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
                     if (i == NQK - 1) read16(vbuf, vrow + 16, vf[1]);
                     __builtin_amdgcn_sched_barrier(0);
                 }
+                asm volatile("" : "+v"(nxt), "+v"(sum));               // (they stay in this block: the compiler would move them down to their use)
                 qs.l += sum;
                 if (pending) {
                     pending = false;
@@ -728,7 +734,6 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
             constexpr std::true_type YES;
             constexpr std::false_type NO;
             const int valid0 = L - t0 * C::T;                          // keys of the first tile on
-            auto next = [](int s) { return s + 1 == C::NS ? 0 : s + 1; };
             // a tile's own slot is over: its V is converted everywhere, its stage free, and tile `need` has arrived everywhere
             auto turn = [&](int x, int s, int need) __attribute__((always_inline)) {
                 if (need < n_pre) wait_for(min(n_pre - 1, x + C::NS - 1) - need);
@@ -743,43 +748,42 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
             read_k(lds, 0, k, ks);
 #pragma unroll
             for (int i = 0; i < NQK; ++i) qk(i, S[0], k, ks);
-            int s = 0, x = 0;                                          // stage of tile x
-            if constexpr (C::U == 2) {
-                read_k(lds, 1, k, ks);
-                check(S[0], valid0, 0);
-                while (true) {
-                    const int vb = (x & 1) * C::VBUF, s1 = next(s), valid = valid0 - x * C::T;
-                    slot(YES, S[0], S[1], P[1], P[0], C::VBUF - vb, 32, s, vb, valid - wave * C::RW);
-                    turn(x, s, x + 1);
-                    read_k(lds + s1 * C::STAGE, 0, k, ks);
+            if constexpr (C::U == 2) read_k(lds, 1, k, ks);
+            else read_k(lds + C::STAGE, 0, k, ks);
+            check(S[0], valid0, 0);
+            // tile x, in stage ST: x % NS, so that every LDS address is a constant away from the lane's; true: it was the last
+            int x = 0;
+            auto one = [&](auto stage) __attribute__((always_inline)) {
+                constexpr int ST = decltype(stage)::value, NEXT = (ST + 1) % C::NS, ODD = ST & 1, VB = ODD * C::VBUF;
+                const int valid = valid0 - x * C::T;
+                if constexpr (C::U == 2) {
+                    slot(YES, S[0], S[1], P[1], P[0], C::VBUF - VB, 32, ST, VB, valid - wave * C::RW);
+                    turn(x, ST, x + 1);
+                    read_k(lds + NEXT * C::STAGE, 0, k, ks);
                     check(S[1], valid, 1);
-                    slot(NO, S[1], S[0], P[0], P[1], vb, 0, 0, 0, 0);
-                    read_k(lds + s1 * C::STAGE, 1, k, ks);
-                    s = s1;
-                    if (++x == n_pre) break;
-                    check(S[0], valid - C::T, 0);
-                }
-                last_pv(P[1], ((n_pre - 1) & 1) * C::VBUF, 32);
-            } else {
-                read_k(lds + C::STAGE, 0, k, ks);
-                check(S[0], valid0, 0);
-                auto one = [&](f32x16_t &cur, f32x16_t &nxt, const u32x4_t (&pp)[2], u32x4_t (&pn)[2], int vb) __attribute__((always_inline)) {
-                    const int s1 = next(s), valid = valid0 - x * C::T;
-                    slot(YES, cur, nxt, pp, pn, C::VBUF - vb, 0, s, vb, valid - wave * C::RW);
-                    turn(x, s, x + 2);
-                    read_k(lds + next(s1) * C::STAGE, 0, k, ks);
-                    s = s1;
+                    slot(NO, S[1], S[0], P[0], P[1], VB, 0, 0, 0, 0);
+                    read_k(lds + NEXT * C::STAGE, 1, k, ks);
                     if (++x == n_pre) return true;
-                    check(nxt, valid - C::T, 0);
-                    return false;
-                };
-                while (true) {
-                    if (one(S[0], S[1], P[1], P[0], 0)) break;
-                    if (one(S[1], S[0], P[0], P[1], C::VBUF)) break;
+                    check(S[0], valid - C::T, 0);
+                } else {
+                    slot(YES, S[ODD], S[1 - ODD], P[1 - ODD], P[ODD], C::VBUF - VB, 0, ST, VB, valid - wave * C::RW);
+                    turn(x, ST, x + 2);
+                    read_k(lds + (NEXT + 1) % C::NS * C::STAGE, 0, k, ks);
+                    if (++x == n_pre) return true;
+                    check(S[1 - ODD], valid - C::T, 0);
                 }
-                if (n_pre & 1) last_pv(P[0], 0, 0);
-                else last_pv(P[1], C::VBUF, 0);
+                return false;
+            };
+            static_assert(C::NS == 4, "the tiles below");
+            while (true) {
+                if (one(std::integral_constant<int, 0>())) break;
+                if (one(std::integral_constant<int, 1>())) break;
+                if (one(std::integral_constant<int, 2>())) break;
+                if (one(std::integral_constant<int, 3>())) break;
             }
+            if constexpr (C::U == 2) last_pv(P[1], ((n_pre - 1) & 1) * C::VBUF, 32);
+            else if (n_pre & 1) last_pv(P[0], 0, 0);
+            else last_pv(P[1], C::VBUF, 0);
         }
         __syncthreads();
 
