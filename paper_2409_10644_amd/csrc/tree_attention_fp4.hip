@@ -170,13 +170,15 @@ __device__ __forceinline__ int anew(int v)
     return v;
 }
 
-// Weights of a pair of scores, packed, and their sum as they are packed (so that numerator and denominator agree).
+// Weights of a pair of scores, packed for the matrix unit, and their sum (in 32 bits; a dot product of the packed ones would occupy
+// the matrix unit: 3 ns each beside it, measured).
 __device__ __forceinline__ void weigh2(const f32x16_t &s, int r, float &sum, u32x4_t *pb)
 {
-    const bf16x2_t one = {(__bf16)1.f, (__bf16)1.f};
-    unsigned u = __builtin_bit_cast(unsigned, (bf16x2_t){(__bf16)fast_exp2(s[r]), (__bf16)fast_exp2(s[r + 1])});
-    asm volatile("" : "+v"(u));      // (stays where it is written, between two matrix instructions)
-    sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, u), one, sum, false);
+    const float a = fast_exp2(s[r]), b = fast_exp2(s[r + 1]);
+    unsigned u = __builtin_bit_cast(unsigned, (bf16x2_t){(__bf16)a, (__bf16)b});
+    sum += a;
+    sum += b;
+    asm volatile("" : "+v"(u), "+v"(sum));      // (stays where it is written, between two matrix instructions)
     pb[r / 8][(r % 8) / 2] = u;
 }
 
@@ -278,7 +280,7 @@ __device__ __forceinline__ int wave_max(int v)
 __device__ __forceinline__ int wave_last(int v) { return __builtin_amdgcn_readlane(v, 63); }
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
-template <int D, int QBP>
+template <int D, int QBP, bool NT>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void tree_attn_fp4_kernel(const Fp4AttnParams args, const int min_tiles)
 {
     const Fp4AttnParams &p = args;
@@ -395,10 +397,27 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         const unsigned char *ksc = (const unsigned char *)p.cache.k_scales + pre / 32, *vsc = (const unsigned char *)p.cache.v_scales + pre / 32;
 
         // a tile's codes and scales into stage s; rows beyond the last key repeat it
-        auto issue = [&](int x, int s) __attribute__((always_inline)) {
+        const uint32_t f_at = f_row * C::RB + f_grp * 16;
+        const int f_row2 = (lane & 31) / C::GR, f_grp2 = ((lane & 31) % C::GR) ^ swz4<D>(f_row2);      // half a load: the upper lanes bring V
+        const unsigned char *const f_half = (g ? vc : kc) + f_row2 * C::RB + f_grp2 * 16, *const f_sc = (g ? vsc : ksc) + sc_idx * 4;
+        auto issue = [&](int x, int at) __attribute__((always_inline)) {
             const int r0 = (t0 + x) * C::T + wave * C::RW, last = L - 1 - r0;        // (may be negative: a wavefront without keys)
-            unsigned char *to = stage0 + s * C::STAGE;
+            unsigned char *to = stage0 + at;
             const int64_t base = (int64_t)r0 * C::RB;
+            if (__builtin_expect(last >= C::RW - 1, 1)) {
+                if constexpr (C::KB >= 1024) {
+                    // (read by one workgroup: not kept in the caches)
+#pragma unroll
+                    for (int i = 0; i < C::KB / 1024; ++i) {
+                        load_to_lds16<NT>(kc + base + i * 1024, f_at, to + i * 1024);
+                        load_to_lds16<NT>(vc + base + i * 1024, f_at, to + C::KB + i * 1024);
+                    }
+                } else {
+                    load_to_lds16_at(f_half + base, to);
+                }
+                load_to_lds4_at(f_sc + (int64_t)r0 * C::SB, to + 2 * C::KB);
+                return;
+            }
             if constexpr (C::KB >= 1024) {
 #pragma unroll
                 for (int i = 0; i < C::KB / 1024; ++i) {
@@ -407,19 +426,15 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
                     load_to_lds16_at(vc + off, to + C::KB + i * 1024);
                 }
             } else {
-                // half a load each: the upper lanes bring V
-                const int l = lane & 31, fr = l / C::GR, fg = (l % C::GR) ^ swz4<D>(fr);
-                const int64_t off = base + (int64_t)min(fr, last) * C::RB + fg * 16;
-                load_to_lds16_at((g ? vc : kc) + off, to);
+                load_to_lds16_at(f_half + base + (int64_t)(min(f_row2, last) - f_row2) * C::RB, to);
             }
-            const int64_t sb = (int64_t)r0 * C::SB + min(sc_idx * 4, (last * C::SB) & ~3);
-            load_to_lds4_at((g ? vsc : ksc) + sb, to + 2 * C::KB);
+            load_to_lds4_at(f_sc + (int64_t)r0 * C::SB + (min(sc_idx * 4, (last * C::SB) & ~3) - sc_idx * 4), to + 2 * C::KB);
         };
         // 16 of this wavefront's V rows, `half` * 16 .. of its stage, of which `valid` exist: the lane's quarter of one, and into
         // the V buffer as bf16, one 16-byte chunk after the other
         struct Codes { unsigned code[D / 32], byte; };
-        auto read_codes = [&](int s, int half, int valid) __attribute__((always_inline)) {
-            const unsigned char *from = stage0 + s * C::STAGE + C::KB;
+        auto read_codes = [&](int at, int half, int valid) __attribute__((always_inline)) {
+            const unsigned char *from = stage0 + at + C::KB;
             const int r = half * 16 + d_row;
             Codes c;
             if constexpr (D == 128) {
@@ -442,8 +457,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
             *(uint4 *)(lds + C::RING + vbuf + (wave * 16 + d_row) * 64 + (D == 128 ? d_unit : d_unit >> 1) * C::VCOLS +
                        (((D == 128 ? i : (d_unit & 1) * 2 + i) ^ vswz(d_row)) * 16)) = fp4x8_to_bf16(c.code[i], fp4_scale(c.byte));
         };
-        auto convert = [&](int s, int half, int vbuf, int valid) __attribute__((always_inline)) {
-            const Codes c = read_codes(s, half, valid);
+        auto convert = [&](int at, int half, int vbuf, int valid) __attribute__((always_inline)) {
+            const Codes c = read_codes(at, half, valid);
 #pragma unroll
             for (int i = 0; i < D / 32; ++i) write_codes(c, i, vbuf);
         };
@@ -468,7 +483,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         uint4 qr[C::ST][4];
         __syncthreads();                                               // (LDS is free: the piece before may have folded in it)
         if (n_pre > 0) issue(0, 0);
-        if (n_pre > 1) issue(1, 1);
+        if (n_pre > 1) issue(1, C::STAGE);
         {
             int node;
             const int64_t q_row = row_of(anew(ln), node);
@@ -479,7 +494,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         }
 #pragma unroll
         for (int x = 2; x < C::AHEAD; ++x)
-            if (x < n_pre) issue(x, x);
+            if (x < n_pre) issue(x, x * C::STAGE);
         Block<D> qs;
 #pragma unroll
         for (int cb = 0; cb < C::CB; ++cb) qs.o[cb] = (f32x16_t){0};
@@ -624,7 +639,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
             int s = 0;                                                 // stage of tile x
             for (int x = 0; x < n_pre; ++x) {
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // (the stage of the tile before has been read)
-                if (x + C::NS - 1 < n_pre) issue(x + C::NS - 1, s == 0 ? C::NS - 1 : s - 1);
+                if (x + C::NS - 1 < n_pre) issue(x + C::NS - 1, (s == 0 ? C::NS - 1 : s - 1) * C::STAGE);
                 wait_for(min(n_pre - 1 - x, C::NS - 1));
                 f32x16_t sacc[1];
                 u32x4_t k[C::ST];
@@ -635,7 +650,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
                 const int valid = L - (t0 + x) * C::T;                 // keys of this tile that exist
                 const uint32_t bits[1] = {exist(valid, 0)};
                 absorb<C>(sacc, qs, g, valid < C::T, bits, [&](int i, bf16x8_t (&vf)[C::CB]) __attribute__((always_inline)) {
-                    convert(s, i, 0, valid - wave * C::RW);
+                    convert(s * C::STAGE, i, 0, valid - wave * C::RW);
                     read16(0, 0, vf);
                 });
                 s = s + 1 == C::NS ? 0 : s + 1;
@@ -647,52 +662,64 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
             u32x4_t P[2][2], k[C::ST];
             int ks = 0;
             float alpha = 1.f;
-            bool pending = false;                                      // (uniform) the output is to be scaled by alpha once block j - 1 is in
+            unsigned pending = 0;                                      // (uniform) the output is to be scaled by alpha once block j - 1 is in
             float limit = qs.m_ref == -INFINITY ? -INFINITY : SLACK;   // what a score may be before the reference moves (none seen yet: any does)
-            // scores of the next block: its missing keys, and the reference where they outgrow it
-            auto check = [&](f32x16_t &s, int valid, int u) __attribute__((always_inline)) {
-                if (valid < C::T) {
-                    const uint32_t own = exist(valid, u) >> (4 * g);
+            auto scale_o = [&]() __attribute__((always_inline)) {
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const uint32_t seen = (uint32_t)__builtin_amdgcn_sbfe((int)own, 8 * (r / 4) + r % 4, 1);
-                        s[r] = __uint_as_float((__float_as_uint(s[r]) & seen) | (0xff800000u & ~seen));
-                    }
-                }
-                float mx = fmaxf(s[0], s[1]);
+                for (int cb = 0; cb < C::CB; ++cb)
 #pragma unroll
-                for (int r = 2; r < 16; r += 2) mx = fmaxf(fmaxf(mx, s[r]), s[r + 1]);
+                    for (int r = 0; r < 16; ++r) qs.o[cb][r] *= alpha;
+                pending = 0;
+            };
+            // Scores of the next block, mx their maximum: its missing keys, and the reference where they outgrow it.  One branch in
+            // the common case, not taken.
+            auto check = [&](f32x16_t &s, float mx, int valid, int u) __attribute__((always_inline)) {
                 // (the other half's keys are looked at when any lane's ask for it)
-                if (__builtin_expect(__builtin_amdgcn_ballot_w64(mx > limit) != 0, 0)) {
+                const unsigned long long over = __builtin_amdgcn_ballot_w64(mx > limit);
+                if (__builtin_expect((unsigned)over | (unsigned)(over >> 32) | pending | (unsigned)(valid - C::T) >> 31, 0)) {
+                    if (pending) scale_o();
+                    if (valid < C::T) {
+                        const uint32_t own = exist(valid, u) >> (4 * g);
+                        mx = -INFINITY;
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) {
+                            const uint32_t seen = (uint32_t)__builtin_amdgcn_sbfe((int)own, 8 * (r / 4) + r % 4, 1);
+                            s[r] = __uint_as_float((__float_as_uint(s[r]) & seen) | (0xff800000u & ~seen));
+                            mx = fmaxf(mx, s[r]);
+                        }
+                    }
                     mx = half_max(mx);
                     const bool none = qs.m_ref == -INFINITY, grow = mx > limit;
-                    const float by = grow ? mx : 0.f;
-                    alpha = grow && none ? 0.f : fast_exp2(-by);
-                    pending = true;
-                    if (grow) {
-                        qs.m_ref = (none ? 0.f : qs.m_ref) + mx;
-                        limit = SLACK;
+                    if (__builtin_amdgcn_ballot_w64(grow) != 0) {
+                        const float by = grow ? mx : 0.f;
+                        alpha = grow && none ? 0.f : fast_exp2(-by);
+                        pending = 1;
+                        if (grow) {
+                            qs.m_ref = (none ? 0.f : qs.m_ref) + mx;
+                            limit = SLACK;
+                        }
+                        qs.l *= alpha;
+                        const float start = qs.m_ref == -INFINITY ? 0.f : -qs.m_ref;
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) qs.start[r] = start;
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) s[r] -= by;
                     }
-                    qs.l *= alpha;
-                    const float start = qs.m_ref == -INFINITY ? 0.f : -qs.m_ref;
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) qs.start[r] = start;
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) s[r] -= by;
                 }
             };
             // weights of `cur` into pn; scores of the next block into nxt; pp times 32 rows of V from `vrow` on into the output;
-            // CONV: this wavefront's share of a tile's V converted on the way.  Beside the last block the scores are of whatever K
+            // CONV: this wavefront's share of a tile's V converted on the way.  Returns the largest score of nxt.  Beside the last block the scores are of whatever K
             // the registers hold, unused; before the first one pp and the V rows are zeros.
             auto slot = [&](auto conv, f32x16_t &cur, f32x16_t &nxt, const u32x4_t (&pp)[2], u32x4_t (&pn)[2], int vbuf, int vrow, int cs, int cbuf,
                             int cvalid) __attribute__((always_inline)) {
                 constexpr bool CONV = decltype(conv)::value;
+                asm volatile("" : "+v"(qs.start));
                 bf16x8_t vf[2][C::CB];
                 read16(vbuf, vrow, vf[0]);
                 Codes cv;
                 if (CONV) cv = read_codes(cs, 0, cvalid);
                 __builtin_amdgcn_sched_barrier(0);
-                float sum = 0.f;
+                float sum = 0.f, mx = -INFINITY;
 #pragma unroll
                 for (int i = 0; i < NQK + NPV; ++i) {
                     if (i < NQK) qk(i, nxt, k, ks);
@@ -708,20 +735,21 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
                         for (int x = 0; x < D / 32; ++x)
                             if ((D == 128 ? 8 : 5) + x == i) write_codes(cv, x, cbuf);
                     }
+#pragma unroll
+                    for (int x = 0; x < 8; ++x)                        // (the scores are whole some matrix instructions after their last)
+                        if ((D == 128 ? 10 + x / 2 : 5 + x / 4) == i) {
+                            mx = fmaxf(fmaxf(mx, nxt[2 * x]), nxt[2 * x + 1]);
+                            asm volatile("" : "+v"(mx));
+                        }
                     if (i == NQK - 1) read16(vbuf, vrow + 16, vf[1]);
                     __builtin_amdgcn_sched_barrier(0);
                 }
-                asm volatile("" : "+v"(nxt), "+v"(sum));               // (they stay in this block: the compiler would move them down to their use)
+                asm volatile("" : "+v"(nxt));                          // (stays in this block: the compiler would move it down to its use)
                 qs.l += sum;
-                if (pending) {
-                    pending = false;
-#pragma unroll
-                    for (int cb = 0; cb < C::CB; ++cb)
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) qs.o[cb][r] *= alpha;
-                }
+                return mx;
             };
             auto last_pv = [&](const u32x4_t (&pp)[2], int vbuf, int vrow) __attribute__((always_inline)) {
+                if (pending) scale_o();
 #pragma unroll
                 for (int hf = 0; hf < 2; ++hf) {
                     bf16x8_t vf[C::CB];
@@ -735,10 +763,16 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
             constexpr std::false_type NO;
             const int valid0 = L - t0 * C::T;                          // keys of the first tile on
             // a tile's own slot is over: its V is converted everywhere, its stage free, and tile `need` has arrived everywhere
-            auto turn = [&](int x, int s, int need) __attribute__((always_inline)) {
-                if (need < n_pre) wait_for(min(n_pre - 1, x + C::NS - 1) - need);
-                meet();
-                if (x + C::NS < n_pre) issue(x + C::NS, s);
+            constexpr int NEED = 3 - C::U;                             // tile x + NEED
+            auto turn = [&](int x, int at) __attribute__((always_inline)) {
+                if (__builtin_expect(x + C::NS < n_pre, 1)) {
+                    MCSD_WAIT_VMCNT((C::NS - 1 - NEED) * C::LPT);
+                    meet();
+                    issue(x + C::NS, at);
+                } else {
+                    if (x + NEED < n_pre) wait_for(n_pre - 1 - x - NEED);
+                    meet();
+                }
             };
 #pragma unroll
             for (int i = 0; i < C::VBUF / 4096; ++i) *(uint4 *)(lds + C::RING + C::VBUF + i * 4096 + anew(tid) * 16) = make_uint4(0, 0, 0, 0);
@@ -750,40 +784,59 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
             for (int i = 0; i < NQK; ++i) qk(i, S[0], k, ks);
             if constexpr (C::U == 2) read_k(lds, 1, k, ks);
             else read_k(lds + C::STAGE, 0, k, ks);
-            check(S[0], valid0, 0);
-            // tile x, in stage ST: x % NS, so that every LDS address is a constant away from the lane's; true: it was the last
-            int x = 0;
-            auto one = [&](auto stage) __attribute__((always_inline)) {
-                constexpr int ST = decltype(stage)::value, NEXT = (ST + 1) % C::NS, ODD = ST & 1, VB = ODD * C::VBUF;
-                const int valid = valid0 - x * C::T;
-                if constexpr (C::U == 2) {
-                    slot(YES, S[0], S[1], P[1], P[0], C::VBUF - VB, 32, ST, VB, valid - wave * C::RW);
-                    turn(x, ST, x + 1);
-                    read_k(lds + NEXT * C::STAGE, 0, k, ks);
-                    check(S[1], valid, 1);
-                    slot(NO, S[1], S[0], P[0], P[1], VB, 0, 0, 0, 0);
-                    read_k(lds + NEXT * C::STAGE, 1, k, ks);
-                    if (++x == n_pre) return true;
-                    check(S[0], valid - C::T, 0);
-                } else {
-                    slot(YES, S[ODD], S[1 - ODD], P[1 - ODD], P[ODD], C::VBUF - VB, 0, ST, VB, valid - wave * C::RW);
-                    turn(x, ST, x + 2);
-                    read_k(lds + (NEXT + 1) % C::NS * C::STAGE, 0, k, ks);
-                    if (++x == n_pre) return true;
-                    check(S[1 - ODD], valid - C::T, 0);
-                }
-                return false;
-            };
-            static_assert(C::NS == 4, "the tiles below");
-            while (true) {
-                if (one(std::integral_constant<int, 0>())) break;
-                if (one(std::integral_constant<int, 1>())) break;
-                if (one(std::integral_constant<int, 2>())) break;
-                if (one(std::integral_constant<int, 3>())) break;
+            {
+                float mx = S[0][0];
+#pragma unroll
+                for (int r = 1; r < 16; ++r) mx = fmaxf(mx, S[0][r]);
+                check(S[0], mx, valid0, 0);
             }
-            if constexpr (C::U == 2) last_pv(P[1], ((n_pre - 1) & 1) * C::VBUF, 32);
-            else if (n_pre & 1) last_pv(P[0], 0, 0);
-            else last_pv(P[1], C::VBUF, 0);
+            int x = 0, at = 0, vb = 0;                                 // tile, its stage's offset, its V buffer's
+            const auto after = [&](int at) { return at + C::STAGE == C::RING ? 0 : at + C::STAGE; };
+            if constexpr (C::U == 2) {
+                while (true) {
+                    const int valid = valid0 - x * C::T, next = after(at);
+                    float mx = slot(YES, S[0], S[1], P[1], P[0], C::VBUF - vb, 32, at, vb, valid - wave * C::RW);
+                    turn(x, at);
+                    read_k(lds + next, 0, k, ks);
+                    check(S[1], mx, valid, 1);
+                    mx = slot(NO, S[1], S[0], P[0], P[1], vb, 0, 0, 0, 0);
+                    read_k(lds + next, 1, k, ks);
+                    if (__builtin_expect(++x == n_pre, 0)) break;
+                    check(S[0], mx, valid - C::T, 0);
+                    at = next;
+                    vb = C::VBUF - vb;
+                }
+                last_pv(P[1], vb, 32);
+            } else {
+                // (a loop of two tiles with one way out, an odd one before it: with two ways out the compiler copies the scores)
+                float mx;
+                auto one = [&](f32x16_t &cur, f32x16_t &nxt, const u32x4_t (&pp)[2], u32x4_t (&pn)[2]) __attribute__((always_inline)) {
+                    const int next = after(at);
+                    mx = slot(YES, cur, nxt, pp, pn, C::VBUF - vb, 0, at, vb, valid0 - x * C::T - wave * C::RW);
+                    turn(x, at);
+                    read_k(lds + after(next), 0, k, ks);
+                    at = next;
+                    vb = C::VBUF - vb;
+                    ++x;
+                };
+                if (n_pre & 1) {
+                    one(S[0], S[1], P[1], P[0]);
+                    if (x < n_pre) check(S[1], mx, valid0 - x * C::T, 0);
+                    S[0] = S[1];
+                    P[1][0] = P[0][0];
+                    P[1][1] = P[0][1];
+                }
+                if (x < n_pre) {
+                    while (true) {
+                        one(S[0], S[1], P[1], P[0]);
+                        check(S[1], mx, valid0 - x * C::T, 0);
+                        one(S[1], S[0], P[0], P[1]);
+                        if (__builtin_expect(x == n_pre, 0)) break;
+                        check(S[0], mx, valid0 - x * C::T, 0);
+                    }
+                }
+                last_pv(P[1], C::VBUF - vb, 0);
+            }
         }
         __syncthreads();
 
@@ -994,7 +1047,9 @@ bool make_plan(int B, int H_kv, int grp, int d, int n_rows, int n, int max_prefi
 template <int D>
 void launch(const Fp4AttnParams &p, const Fp4Plan &pl, hipStream_t st)
 {
-    auto kernel = pl.QBP == 1 ? tree_attn_fp4_kernel<D, 1> : pl.QBP == 2 ? tree_attn_fp4_kernel<D, 2> : tree_attn_fp4_kernel<D, 4>;
+    // (only with 128 rows to a chunk can there be more than one)
+    auto kernel = pl.QBP == 1 ? tree_attn_fp4_kernel<D, 1, true> : pl.QBP == 2 ? tree_attn_fp4_kernel<D, 2, true>
+                  : pl.chunks == 1 ? tree_attn_fp4_kernel<D, 4, true> : tree_attn_fp4_kernel<D, 4, false>;
     mcsd_launch(MCSD_KERNEL_ATTN_SWEEP, kernel, dim3(pl.workgroups), dim3(256), st, p, pl.min_tiles);
 }
 
