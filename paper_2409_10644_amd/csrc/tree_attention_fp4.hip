@@ -304,6 +304,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         }
     };
     fetch(0);
+    const bool prepared = p.ws_tag && uniform((int)*p.ws_tag) == (int)WS_TAG;
     int total = 0, most = 0;                                           // tiles of one unit of every sequence
     for (int b0 = 0; b0 < p.B; b0 += 64) {
         if (b0) fetch(b0);
@@ -318,13 +319,18 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         if (per >= most) {
             aligned = per;
         } else if (p.B <= 64) {
-            // the smallest size whose splits fit the grid; lanes try one each
-            const int cand = per + lane * (1 + per / 64), t = len_l >= 0 ? tiles_of(len_l) : 0;
-            int splits = 0;
-            for (int b = 0; b < p.B; ++b) splits += (__builtin_amdgcn_readlane(t, b) + cand - 1) / cand;
-            const unsigned long long fits = __builtin_amdgcn_ballot_w64(splits * p.units <= p.workgroups);
-            if (fits) aligned = __builtin_amdgcn_readlane(cand, __builtin_ctzll(fits));
-            if (aligned > per + per / 8 + 2) aligned = 0;
+            // the smallest size whose splits fit the grid, unless it is much more than an equal piece
+            const int t = len_l >= 0 ? tiles_of(len_l) : 0;
+            auto fits = [&](int size) { return wave_last(wave_scan((t + size - 1) / size)) * p.units <= p.workgroups; };
+            int lo = per, hi = per + per / 8 + 2;
+            if (fits(hi)) {
+                while (lo < hi) {
+                    const int mid = (lo + hi) >> 1;
+                    if (fits(mid)) hi = mid;
+                    else lo = mid + 1;
+                }
+                aligned = hi;
+            }
         }
     }
     if (aligned) per = aligned;
@@ -352,7 +358,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         }
         if (b < 0) return;
     }
-    int64_t done = (int64_t)w * per;                                   // flat: tiles before this one
+    int done = w * per;                                                // flat: tiles before this one
 
     // ---- what stays the same for all pairs ----
     const int chunk_rows = 32 * QBP, n_rows = p.n - p.row0;
@@ -764,7 +770,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
             const int valid0 = L - t0 * C::T;                          // keys of the first tile on
             // a tile's own slot is over: its V is converted everywhere, its stage free, and tile `need` has arrived everywhere
             constexpr int NEED = 3 - C::U;                             // tile x + NEED
+            // Of two workgroups on a compute unit the older one would always go first, and the other be alone at the end, at half
+            // the rate: they take turns of four tiles instead (which is which makes no difference to any result).
+            const int late = 2 * w >= p.workgroups;
             auto turn = [&](int x, int at) __attribute__((always_inline)) {
+                if (((x >> 2) ^ late) & 1) __builtin_amdgcn_s_setprio(1);
+                else __builtin_amdgcn_s_setprio(0);
                 if (__builtin_expect(x + C::NS < n_pre, 1)) {
                     MCSD_WAIT_VMCNT((C::NS - 1 - NEED) * C::LPT);
                     meet();
@@ -837,6 +848,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
                 }
                 last_pv(P[1], C::VBUF - vb, 0);
             }
+            __builtin_amdgcn_s_setprio(0);
         }
         __syncthreads();
 
@@ -912,10 +924,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
             } else {
                 // ---- one of several pieces: leave it in the workspace; whoever is last folds them in order ----
                 if (!aligned) {
-                    first_piece = (int)((done - tile) / per);
-                    n_pieces = (int)((done - tile + all - 1) / per) - first_piece + 1;
+                    first_piece = (done - tile) / per;
+                    n_pieces = (done - tile + all - 1) / per - first_piece + 1;
                 }
-                if (__hip_atomic_load(p.ws_tag, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != WS_TAG) {
+                first_piece = uniform(first_piece);
+                n_pieces = uniform(n_pieces);
+                if (!prepared) {
 #pragma unroll
                     for (int x = 0; x < C::PP; ++x) acc[x] = (f32x4_t){NAN, NAN, NAN, NAN};
                     write_out(1.f);                                        // never prepared: its counters mean nothing
