@@ -51,7 +51,7 @@ struct Fp4AttnParams {
     int32_t chunks;                  // workgroup units per key/value head
     int32_t units;                   // per sequence: H_kv * chunks
     RowDiv by_units, by_chunks, by_nrows;
-    int32_t workgroups;              // of the launch: pieces that can be
+    int32_t workgroups, single;      // of the launch: pieces that can be; compute units
     float c;                         // softmax scale * log2(e)
     const uint32_t *ws_tag;
     unsigned long long *ctr;         // arrivals of the pair that begins in piece w: ctr[w * CTR_STRIDE], zero before and after every launch
@@ -101,6 +101,8 @@ struct Cfg {
     static constexpr int NS = OWN ? (D == 128 ? 3 : 4) : 4;            // stages; two workgroups per compute unit have 80 KB each
     static constexpr int AHEAD = OWN ? NS - 1 : NS;  // tiles requested before the first is used
     static constexpr int RING = NS * STAGE;
+    static constexpr int MIN_TILES = QBP == 1 ? 2 : QBP == 2 ? 4 : 8;
+    static constexpr float FOLD = QBP == 1 ? 0.5f : QBP == 2 ? 1.f : 2.f;
     static constexpr int PP = CB * 4 / KG;           // pieces (four columns of a row per lane) that a wavefront ends up with
     static constexpr int XCHG = (KG - 1) * QBP * 32 * D * 4;
     static constexpr int LDS = RING + NV * VBUF > XCHG + 4 * 256 + 16 ? RING + NV * VBUF : XCHG + 4 * 256 + 16;
@@ -281,7 +283,7 @@ __device__ __forceinline__ int wave_last(int v) { return __builtin_amdgcn_readla
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
 template <int D, int QBP, bool NT>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void tree_attn_fp4_kernel(const Fp4AttnParams args, const int min_tiles)
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void tree_attn_fp4_kernel(const Fp4AttnParams args)
 {
     const Fp4AttnParams &p = args;
     using C = Cfg<D, QBP>;
@@ -312,17 +314,24 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         total += wave_last(wave_scan(t));
         most = max(most, wave_max(t));
     }
-    int per = max((total * p.units + p.workgroups - 1) / p.workgroups, min_tiles);       // tiles of a piece
-    per = max(per, (most + MAX_SPLITS - 1) / MAX_SPLITS);
-    int aligned = 0;                                                   // > 0: splits of that many tiles, no piece crosses a pair
-    if (p.B * p.units <= p.workgroups) {
+    // One workgroup per compute unit goes through its tiles 1.4 to 1.7 times as fast as one of two, and half as many pieces are half
+    // as much to exchange: two only where each has more than so many tiles (or where pieces would cross pairs otherwise).
+    constexpr int WORTH = QBP == 4 ? 24 : QBP == 2 ? 10 : 8;
+    // Tiles of a piece: no fewer than make its share of the exchange worth while.  Of t tiles in pieces of s, s are one after the
+    // other, and so are the t / s parts that the last one folds: the sum is least at a multiple of sqrt(t).
+    const int least = max(max(C::MIN_TILES, (int)(C::FOLD * __builtin_amdgcn_sqrtf((float)most))), (most + MAX_SPLITS - 1) / MAX_SPLITS);
+    int per = 0, aligned = 0;                                          // aligned > 0: pieces of at most that many tiles, none crosses a pair
+    for (int all = total * p.units >= 2 * p.single * WORTH; all < 2 && !aligned; ++all) {
+        const int resident = all ? p.workgroups : min(p.single, p.workgroups);
+        per = max((total * p.units + resident - 1) / resident, least);
+        if (p.B * p.units > resident) continue;
         if (per >= most) {
             aligned = per;
         } else if (p.B <= 64) {
-            // the smallest size whose splits fit the grid, unless it is much more than an equal piece
+            // the smallest size whose splits fit the grid, unless it is so much more than an equal piece that crossing costs less
             const int t = len_l >= 0 ? tiles_of(len_l) : 0;
-            auto fits = [&](int size) { return wave_last(wave_scan((t + size - 1) / size)) * p.units <= p.workgroups; };
-            int lo = per, hi = per + per / 8 + 2;
+            auto fits = [&](int size) { return wave_last(wave_scan((t + size - 1) / size)) * p.units <= resident; };
+            int lo = per, hi = per + per / 8 + (QBP == 1 ? 12 : 8);
             if (fits(hi)) {
                 while (lo < hi) {
                     const int mid = (lo + hi) >> 1;
@@ -350,9 +359,15 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
                 b = b0 + l;
                 unit = after / e;
                 const int in = after - unit * e;
-                tile = aligned ? in * per : in;
-                left = aligned ? min(per, t_l - tile) : per;
-                if (aligned) { n_pieces = e; first_piece = w - in; }
+                tile = in;
+                left = per;
+                if (aligned) {                                         // as equal as they can be
+                    const int size = t_l / e, more = t_l - size * e;
+                    tile = in * size + min(in, more);
+                    left = size + (in < more);
+                    n_pieces = e;
+                    first_piece = w - in;
+                }
             }
             before = wave_last(upto);
         }
@@ -772,7 +787,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
             constexpr int NEED = 3 - C::U;                             // tile x + NEED
             // Of two workgroups on a compute unit the older one would always go first, and the other be alone at the end, at half
             // the rate: they take turns of four tiles instead (which is which makes no difference to any result).
-            const int late = 2 * w >= p.workgroups;
+            const int late = w >= p.single;
             auto turn = [&](int x, int at) __attribute__((always_inline)) {
                 if (((x >> 2) ^ late) & 1) __builtin_amdgcn_s_setprio(1);
                 else __builtin_amdgcn_s_setprio(0);
@@ -1012,7 +1027,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 
 // ---------------------------------------------------------------------------------------------------- host
 struct Fp4Plan {
-    int QBP, chunks, units, workgroups, min_tiles;
+    int QBP, chunks, units, workgroups, single;
     size_t bytes;                    // workspace
 };
 
@@ -1045,10 +1060,11 @@ bool make_plan(int B, int H_kv, int grp, int d, int n_rows, int n, int max_prefi
     if (rows > 0x3fffffff || units * B > 0x3fffffff || units * B * tiles > 0x3fffffff) return false;
     pl.chunks = (int)chunks;
     pl.units = (int)units;
-    pl.min_tiles = pl.QBP == 1 ? 2 : 4;
-    int most = 2 * compute_units();
+    const int min_tiles = pl.QBP == 1 ? Cfg<128, 1>::MIN_TILES : pl.QBP == 2 ? Cfg<128, 2>::MIN_TILES : Cfg<128, 4>::MIN_TILES;
+    pl.single = compute_units();
+    int most = 2 * pl.single;
     if (most > MAX_PIECES) most = MAX_PIECES;
-    const int64_t pairs = units * B, pieces = pairs * ((tiles + pl.min_tiles - 1) / pl.min_tiles);
+    const int64_t pairs = units * B, pieces = pairs * ((tiles + min_tiles - 1) / min_tiles);
     pl.workgroups = (int)(pieces < most ? pieces : most);
     pl.bytes = 0;
     if (pieces > pairs || pairs > most) {
@@ -1064,7 +1080,7 @@ void launch(const Fp4AttnParams &p, const Fp4Plan &pl, hipStream_t st)
     // (only with 128 rows to a chunk can there be more than one)
     auto kernel = pl.QBP == 1 ? tree_attn_fp4_kernel<D, 1, true> : pl.QBP == 2 ? tree_attn_fp4_kernel<D, 2, true>
                   : pl.chunks == 1 ? tree_attn_fp4_kernel<D, 4, true> : tree_attn_fp4_kernel<D, 4, false>;
-    mcsd_launch(MCSD_KERNEL_ATTN_SWEEP, kernel, dim3(pl.workgroups), dim3(256), st, p, pl.min_tiles);
+    mcsd_launch(MCSD_KERNEL_ATTN_SWEEP, kernel, dim3(pl.workgroups), dim3(256), st, p);
 }
 
 }  // namespace
@@ -1116,7 +1132,7 @@ extern "C" int mcsd_tree_attention_fp4kv(const mcsd_mask_view_t *mask, int32_t B
     p.B = B; p.H_q = H_q; p.H_kv = H_kv; p.grp = H_q / H_kv; p.n = n; p.row0 = row_begin; p.max_prefix = max_prefix;
     p.rows = p.grp * (n - row_begin); p.chunks = pl.chunks; p.units = pl.units;
     p.by_units = row_div_of((uint32_t)pl.units); p.by_chunks = row_div_of((uint32_t)pl.chunks); p.by_nrows = row_div_of((uint32_t)(n - row_begin));
-    p.workgroups = pl.workgroups;
+    p.workgroups = pl.workgroups; p.single = pl.single;
     p.c = softmax_scale * 1.4426950408889634f;
     if (pl.bytes > 0) {
         char *ws = (char *)workspace;
