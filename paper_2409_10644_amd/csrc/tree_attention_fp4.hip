@@ -280,6 +280,12 @@ __device__ __forceinline__ int wave_max(int v)
     return __builtin_amdgcn_readlane(v, 63);
 }
 __device__ __forceinline__ int wave_last(int v) { return __builtin_amdgcn_readlane(v, 63); }
+// n / d for 0 <= n < 2^30, d > 0 and a quotient below 2^20: rounded to 24 bits twice it is off by less than one.
+__device__ __forceinline__ int small_div(int n, int d)
+{
+    const int q = (int)((float)n * __builtin_amdgcn_rcpf((float)d)), r = n - q * d;
+    return q + (r >= d) - (r < 0);
+}
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
 template <int D, int QBP, bool NT>
@@ -330,7 +336,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         } else if (p.B <= 64) {
             // the smallest size whose splits fit the grid, unless it is so much more than an equal piece that crossing costs less
             const int t = len_l >= 0 ? tiles_of(len_l) : 0;
-            auto fits = [&](int size) { return wave_last(wave_scan((t + size - 1) / size)) * p.units <= resident; };
+            auto fits = [&](int size) { return wave_last(wave_scan(small_div(t + size - 1, size))) * p.units <= resident; };
             int lo = per, hi = per + per / 8 + (QBP == 1 ? 12 : 8);
             if (fits(hi)) {
                 while (lo < hi) {
@@ -350,14 +356,14 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         for (int b0 = 0; b0 < p.B && b < 0; b0 += 64) {
             if (b0 != b_lanes) fetch(b0);
             const int t = len_l >= 0 ? tiles_of(len_l) : 0;
-            const int each = aligned ? (t + per - 1) / per : t;        // per unit: splits, or tiles
+            const int each = aligned ? small_div(t + per - 1, per) : t;        // per unit: splits, or tiles
             const int upto = before + wave_scan(each * p.units);
             const unsigned long long mine = __builtin_amdgcn_ballot_w64(upto > here);
             if (mine) {
                 const int l = __builtin_ctzll(mine), e = __builtin_amdgcn_readlane(each, l), t_l = __builtin_amdgcn_readlane(t, l);
                 const int after = here - (__builtin_amdgcn_readlane(upto, l) - e * p.units);
                 b = b0 + l;
-                unit = after / e;
+                unit = uniform(small_div(after, e));
                 const int in = after - unit * e;
                 tile = in;
                 left = per;
