@@ -6,6 +6,9 @@
 // or three exchanges between neighbouring lanes.  The sines and cosines of a row serve all its heads: they are computed once per
 // workgroup, one angle per lane, and shared through LDS.  Angles are products in binary64, reduced to a fraction of a turn there,
 // so position 10^6 is as exact as position 1.
+//
+// Bound by memory: prompts of 500 to 2000 tokens of 48 heads of 128 channels in bf16 (123 MB read and written) take 26 to 28 us,
+// 4.4 to 4.7 TB/s where a large copy runs at 4.9; the 44 tree nodes of one sequence take 4.3 us, a launch and two trips to memory.
 #include "fp4_format.h"
 
 namespace {
@@ -194,7 +197,10 @@ int qk_call(const mcsd_mask_view_t *mask, mcsd_dtype_t dtype, int32_t B, int32_t
         for (int l = 0; l < mask->gamma; ++l) p.off[l] = mask->level_off_host[l];
     }
     p.by_heads = row_div_of((uint32_t)p.heads);
-    if ((int64_t)rows * B > 2048) launch<4>(p, d, dtype == MCSD_F32, B, (hipStream_t)hip_stream);
+    // Four rows per workgroup where one leaves lanes idle (64000 rows of 12 heads: 73 us, one by one 101; 8000 of 12: 11.0, 13.3),
+    // unless there are so few that the workgroups count (2000 rows of 12: 5.5, one by one 4.9).  With whole rows of lanes one by
+    // one is the faster (5000 rows of 48 heads: 27.0 us, four at a time 28.9; 44 of 96: 4.3, 9.4).
+    if (p.heads * (d / 16) < 256 && (int64_t)rows * B > 2048) launch<4>(p, d, dtype == MCSD_F32, B, (hipStream_t)hip_stream);
     else launch<1>(p, d, dtype == MCSD_F32, B, (hipStream_t)hip_stream);
     return mcsd_hip_status(hipGetLastError());
 }

@@ -50,7 +50,7 @@ struct Fp4AttnParams {
     int32_t rows;                    // query rows per key/value head: grp * (n - row0)
     int32_t chunks;                  // workgroup units per key/value head
     int32_t units;                   // per sequence: H_kv * chunks
-    RowDiv by_units, by_chunks, by_nrows;
+    RowDiv by_chunks, by_nrows;
     int32_t workgroups, single;      // of the launch: pieces that can be; compute units
     float c;                         // softmax scale * log2(e)
     const uint32_t *ws_tag;
@@ -1137,7 +1137,7 @@ extern "C" int mcsd_tree_attention_fp4kv(const mcsd_mask_view_t *mask, int32_t B
     p.node_stride = node_stride; p.head_stride = head_stride; p.mask_words = mask->words_per_row;
     p.B = B; p.H_q = H_q; p.H_kv = H_kv; p.grp = H_q / H_kv; p.n = n; p.row0 = row_begin; p.max_prefix = max_prefix;
     p.rows = p.grp * (n - row_begin); p.chunks = pl.chunks; p.units = pl.units;
-    p.by_units = row_div_of((uint32_t)pl.units); p.by_chunks = row_div_of((uint32_t)pl.chunks); p.by_nrows = row_div_of((uint32_t)(n - row_begin));
+    p.by_chunks = row_div_of((uint32_t)pl.chunks); p.by_nrows = row_div_of((uint32_t)(n - row_begin));
     p.workgroups = pl.workgroups; p.single = pl.single;
     p.c = softmax_scale * 1.4426950408889634f;
     if (pl.bytes > 0) {
