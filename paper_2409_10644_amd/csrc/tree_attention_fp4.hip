@@ -788,15 +788,15 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
             };
             constexpr std::true_type YES;
             constexpr std::false_type NO;
-            const int valid0 = L - t0 * C::T;                          // keys of the first tile on
+            const int valid0 = min(L, t1 * C::T) - t0 * C::T;          // keys of the piece
             // a tile's own slot is over: its V is converted everywhere, its stage free, and tile `need` has arrived everywhere
             constexpr int NEED = 3 - C::U;                             // tile x + NEED
             // Of two workgroups on a compute unit the older one would always go first, and the other be alone at the end, at half
             // the rate: they take turns of four tiles instead (which is which makes no difference to any result).
-            const int late = w >= p.single;
+            // (A branch that the compiler does not see: it would copy accumulators along its two ways.)
+            const int late = w >= p.single ? 4 : 0;
             auto turn = [&](int x, int at) __attribute__((always_inline)) {
-                if (((x >> 2) ^ late) & 1) __builtin_amdgcn_s_setprio(1);
-                else __builtin_amdgcn_s_setprio(0);
+                asm volatile("s_setprio 0\n\ts_bitcmp0_b32 %0, 2\n\ts_cbranch_scc1 .Lturn%=\n\ts_setprio 1\n.Lturn%=:" : : "s"(x ^ late) : "scc");
                 if (__builtin_expect(x + C::NS < n_pre, 1)) {
                     MCSD_WAIT_VMCNT((C::NS - 1 - NEED) * C::LPT);
                     meet();
@@ -840,7 +840,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
                 }
                 last_pv(P[1], vb, 32);
             } else {
-                // (a loop of two tiles with one way out, an odd one before it: with two ways out the compiler copies the scores)
+                // (two tiles per turn of the loop, the way out at its end: elsewhere the compiler copies the output at every turn.
+                // After an odd number of tiles comes one without keys, and the last look at the reference finds none.)
                 float mx;
                 auto one = [&](f32x16_t &cur, f32x16_t &nxt, const u32x4_t (&pp)[2], u32x4_t (&pn)[2]) __attribute__((always_inline)) {
                     const int next = after(at);
@@ -851,21 +852,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
                     vb = C::VBUF - vb;
                     ++x;
                 };
-                if (n_pre & 1) {
+                while (true) {
                     one(S[0], S[1], P[1], P[0]);
-                    if (x < n_pre) check(S[1], mx, valid0 - x * C::T, 0);
-                    S[0] = S[1];
-                    P[1][0] = P[0][0];
-                    P[1][1] = P[0][1];
-                }
-                if (x < n_pre) {
-                    while (true) {
-                        one(S[0], S[1], P[1], P[0]);
-                        check(S[1], mx, valid0 - x * C::T, 0);
-                        one(S[1], S[0], P[0], P[1]);
-                        if (__builtin_expect(x == n_pre, 0)) break;
-                        check(S[0], mx, valid0 - x * C::T, 0);
-                    }
+                    check(S[1], mx, valid0 - x * C::T, 0);
+                    one(S[1], S[0], P[0], P[1]);
+                    check(S[0], mx, valid0 - x * C::T, 0);
+                    if (__builtin_expect(x >= n_pre, 0)) break;
                 }
                 last_pv(P[1], C::VBUF - vb, 0);
             }
