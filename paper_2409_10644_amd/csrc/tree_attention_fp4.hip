@@ -14,9 +14,21 @@
 // delivers V^T operands to all of them.
 //
 // Codes and scales stream from HBM straight into a ring of LDS stages.  The work is the tiles of all (sequence, head) pairs laid
-// end to end, the tree's own keys first in each, cut into equal pieces for the workgroups that are resident at once, or, where
-// that is as even, into equal pieces of each pair.  A pair's pieces leave their unnormalised output, maximum and sum in the
+// end to end, the tree's own keys first in each, cut into pieces: equal ones of each pair where they fit the workgroups that are
+// resident at once, else equal pieces of the whole.  A pair's pieces leave their unnormalised output, maximum and sum in the
 // workspace, and the workgroup that is last to do so folds them.
+//
+// With more than 32 rows, blocks of 32 keys go through a pipeline: between the matrix instructions that make the scores of one and
+// add the one before it to the output stand the exponentials of the one in the middle; all that happens rarely (a reference that is
+// outgrown, the last keys of a sequence) is behind one branch per block, which is not taken.
+//
+// What bounds it: 120 rows on 8 x 32 heads of 16384 keys take 260 us, 990 TFLOP/s of the products as defined (a large bf16 matrix
+// product of this card: 1200), and 300 when repeated without a pause: the clock falls to 1.85 GHz under the matrix unit's load, a
+// loop of nothing but these 14 instructions per block takes 160.  With all operands zero the same work takes 226.  240 rows of 4
+// heads on 16 x 8 key heads of 512 to 4096 keys take 60 us (36 GFLOP), 44 rows on 32 heads of 1024 keys 18.5, most of it the way to
+// the first key (5 us) and from the last one through the exchange (6 us).  One token of 4 heads on 32 x 8 key heads of 777 to 8191
+// keys takes 45 us for 156 MB, 3.5 TB/s; while all workgroups are in their loops the cache streams at 5.2 to 5.7.  The smallest
+// call takes 7.7 us, a chain of trips to memory: lengths, queries, tree rows, prefix.
 #include <math.h>
 
 #include <atomic>
@@ -102,7 +114,7 @@ struct Cfg {
     static constexpr int AHEAD = OWN ? NS - 1 : NS;  // tiles requested before the first is used
     static constexpr int RING = NS * STAGE;
     static constexpr int MIN_TILES = QBP == 1 ? 2 : QBP == 2 ? 4 : 8;
-    static constexpr float FOLD = QBP == 1 ? 0.5f : QBP == 2 ? 1.f : 2.f;
+    static constexpr float FOLD = QBP == 4 ? 2.f : 0.5f;
     static constexpr int PP = CB * 4 / KG;           // pieces (four columns of a row per lane) that a wavefront ends up with
     static constexpr int XCHG = (KG - 1) * QBP * 32 * D * 4;
     static constexpr int LDS = RING + NV * VBUF > XCHG + 4 * 256 + 16 ? RING + NV * VBUF : XCHG + 4 * 256 + 16;
@@ -321,10 +333,16 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         most = max(most, wave_max(t));
     }
     // One workgroup per compute unit goes through its tiles 1.4 to 1.7 times as fast as one of two, and half as many pieces are half
-    // as much to exchange: two only where each has more than so many tiles (or where pieces would cross pairs otherwise).
-    constexpr int WORTH = QBP == 4 ? 24 : QBP == 2 ? 10 : 8;
+    // as much to exchange: two only where each has more than so many tiles (or where pieces would cross pairs otherwise).  Measured,
+    // one and two, in us: 60 nodes x 4 heads on 16 x 8 key heads of 512 keys 26.5 and 34.8, of 2048 56.4 and 57.0, of 4096 94.8 and
+    // 87; 44 nodes on 8 x 32 key heads of 1024 keys 24.8 and 30.9, of 4096 60 and 57; one token x 4 heads on 32 x 8 key heads of
+    // 1024 keys 20.2 and 24.0, of 4096 47.7 and 42.5.
+    constexpr int WORTH = QBP == 1 ? 8 : 24;
     // Tiles of a piece: no fewer than make its share of the exchange worth while.  Of t tiles in pieces of s, s are one after the
-    // other, and so are the t / s parts that the last one folds: the sum is least at a multiple of sqrt(t).
+    // other, and so are the t / s parts that the last one folds: the sum is least at a multiple of sqrt(t).  (120 nodes on 4 key
+    // heads of 16384 keys, 257 tiles: pieces of 9 take 77 us, of 16 62.2, of 32 61.4; of 4096 keys: of 8 39.0, of 16 38.4, of 32
+    // 43.5.  44 nodes on the same: of 8 28.4 and 22.2, of 16 29.8 and 23.4.  One token on 8 key heads of 4096 keys, 33 tiles: of 2
+    // 16.9, of 4 17.8, of 8 19.5.)
     const int least = max(max(C::MIN_TILES, (int)(C::FOLD * __builtin_amdgcn_sqrtf((float)most))), (most + MAX_SPLITS - 1) / MAX_SPLITS);
     int per = 0, aligned = 0;                                          // aligned > 0: pieces of at most that many tiles, none crosses a pair
     for (int all = total * p.units >= 2 * p.single * WORTH; all < 2 && !aligned; ++all) {
@@ -334,7 +352,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         if (per >= most) {
             aligned = per;
         } else if (p.B <= 64) {
-            // the smallest size whose splits fit the grid, unless it is so much more than an equal piece that crossing costs less
+            // The smallest size whose splits fit the grid, unless it is so much more than an equal piece that crossing costs less.
+            // (A piece of the next pair starts from nothing: 15 to 20 us.  The batch of 16 sequences of 512 to 4096 keys under 60
+            // nodes takes 62 us in pieces of 24 tiles and 70 in equal ones of 19; 32 of 777 to 8191 keys with a token each 48.5, 53.)
             const int t = len_l >= 0 ? tiles_of(len_l) : 0;
             auto fits = [&](int size) { return wave_last(wave_scan(small_div(t + size - 1, size))) * p.units <= resident; };
             int lo = per, hi = per + per / 8 + (QBP == 1 ? 12 : 8);
