@@ -369,20 +369,42 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         }
     }
     if (aligned) per = aligned;
-    int b = -1, unit = 0, tile = 0, n_pieces = 1, first_piece = 0, left = 0;
+    int b = -1, unit = 0, tile = 0, n_pieces = 1, first_piece = 0, left = 0, number = w;
     {
-        int before = 0;
-        const int here = aligned ? w : w * per;
+        int before = 0, t = len_l >= 0 ? tiles_of(len_l) : 0, each = aligned ? small_div(t + per - 1, per) : t, seq = lane;
+        if (aligned && p.B <= 64) {
+            // Pieces of different sizes, two to a compute unit: the sequences by the size of their pieces, the first half of the
+            // workgroups takes them from the largest on, the second half from the smallest on (workgroups come to the compute
+            // units in turn, so the longest piece shares with the shortest).
+            const int pieces = wave_last(wave_scan(each * p.units));
+            if (pieces > p.single) {
+                const int size = each > 0 ? small_div(t + each - 1, each) : 0;
+                int rank = 0;
+                for (int o = 0; o < p.B; ++o) {
+                    const int other = __builtin_amdgcn_readlane(size, o);
+                    rank += other > size || (other == size && o < lane);
+                }
+                rank = 4 * (lane < p.B ? rank : lane);
+                t = __builtin_amdgcn_ds_permute(rank, t);
+                each = __builtin_amdgcn_ds_permute(rank, each);
+                seq = __builtin_amdgcn_ds_permute(rank, lane);
+                if (w >= p.single) number = pieces - 1 - (w - p.single);
+                if (w >= p.single && number < p.single) return;
+            }
+        }
+        const int here = aligned ? number : w * per;
         for (int b0 = 0; b0 < p.B && b < 0; b0 += 64) {
-            if (b0 != b_lanes) fetch(b0);
-            const int t = len_l >= 0 ? tiles_of(len_l) : 0;
-            const int each = aligned ? small_div(t + per - 1, per) : t;        // per unit: splits, or tiles
+            if (p.B > 64) {
+                if (b0 != b_lanes) fetch(b0);
+                t = len_l >= 0 ? tiles_of(len_l) : 0;
+                each = aligned ? small_div(t + per - 1, per) : t;      // per unit: splits, or tiles
+            }
             const int upto = before + wave_scan(each * p.units);
             const unsigned long long mine = __builtin_amdgcn_ballot_w64(upto > here);
             if (mine) {
                 const int l = __builtin_ctzll(mine), e = __builtin_amdgcn_readlane(each, l), t_l = __builtin_amdgcn_readlane(t, l);
                 const int after = here - (__builtin_amdgcn_readlane(upto, l) - e * p.units);
-                b = b0 + l;
+                b = b0 + __builtin_amdgcn_readlane(seq, l);
                 unit = uniform(small_div(after, e));
                 const int in = after - unit * e;
                 tile = in;
@@ -392,7 +414,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
                     tile = in * size + min(in, more);
                     left = size + (in < more);
                     n_pieces = e;
-                    first_piece = w - in;
+                    first_piece = number - in;
                 }
             }
             before = wave_last(upto);
@@ -970,7 +992,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
                     const int ln = anew(tid) & 31, g = (anew(tid) >> 5) & 1;
                     // slot of the piece: a workgroup leaves at most two, the first of them the end of a pair that began before
                     const auto slot_of = [&](int i) { return (int64_t)(2 * (first_piece + i) + (i == 0)); };
-                    const int64_t slot = slot_of(w - first_piece);
+                    const int64_t slot = slot_of(number - first_piece);
                     constexpr int AGENT = 16;                              // (sc1: past this die's L2, for the other dies)
                     constexpr int ROWS = 32 * QBP;
                     if (mine) {
