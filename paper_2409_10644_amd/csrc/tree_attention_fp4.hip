@@ -27,7 +27,7 @@
 // loop of nothing but these 14 instructions per block takes 160.  With all operands zero the same work takes 226.  240 rows of 4
 // heads on 16 x 8 key heads of 512 to 4096 keys take 60 us (36 GFLOP), 44 rows on 32 heads of 1024 keys 18.5, most of it the way to
 // the first key (5 us) and from the last one through the exchange (6 us).  One token of 4 heads on 32 x 8 key heads of 777 to 8191
-// keys takes 42 us for 157 MB, 3.7 TB/s; while all workgroups are in their loops the cache streams at 5.2 to 5.7.  The smallest
+// keys takes 41 us for 157 MB, 3.8 TB/s; while all workgroups are in their loops the cache streams at 5.2 to 5.7.  The smallest
 // call takes 7.7 us, a chain of trips to memory: lengths, queries, tree rows, prefix.
 #include <math.h>
 
@@ -552,8 +552,6 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         // The queries as they are: channels 64 st + 32 g + 8 i .. +7 (also the order of the contraction with the tree's keys).
         uint4 qr[C::ST][4];
         __syncthreads();                                               // (LDS is free: the piece before may have folded in it)
-        if (n_pre > 0) issue(0, 0);
-        if (n_pre > 1) issue(1, C::STAGE);
         {
             int node;
             const int64_t q_row = row_of(anew(ln), node);
@@ -562,9 +560,6 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 #pragma unroll
                 for (int i = 0; i < 4; ++i) qr[st][i] = ((const uint4 *)(p.q + q_row + st * 64 + g * 32))[i];
         }
-#pragma unroll
-        for (int x = 2; x < C::AHEAD; ++x)
-            if (x < n_pre) issue(x, x * C::STAGE);
         Block<D> qs;
 #pragma unroll
         for (int cb = 0; cb < C::CB; ++cb) qs.o[cb] = (f32x16_t){0};
@@ -677,6 +672,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
+        // (The first tiles are requested only now: the compiler's waits for queries and tree rows would be waits for them too, and at
+        // the start all workgroups' requests queue for memory together.  One token for 32 sequences of 777 to 8191 keys 42.4 us
+        // instead of 45, 60 nodes on 16 x 8 key heads of 512 to 4096 keys 59.6 instead of 62.)
+#pragma unroll
+        for (int x = 0; x < C::AHEAD; ++x)
+            if (x < n_pre) issue(x, x * C::STAGE);
         // ---- the prefix ----
         // (a register of their own from here on: what stands in the way before and after may be kept in memory, not in the loops)
 #pragma unroll
