@@ -25,8 +25,8 @@
 // What bounds it: 120 rows on 8 x 32 heads of 16384 keys take 260 us, 990 TFLOP/s of the products as defined (a large bf16 matrix
 // product of this card: 1200), and 300 when repeated without a pause: the clock falls to 1.85 GHz under the matrix unit's load, a
 // loop of nothing but these 14 instructions per block takes 160.  With all operands zero the same work takes 226.  240 rows of 4
-// heads on 16 x 8 key heads of 512 to 4096 keys take 60 us (36 GFLOP), 44 rows on 32 heads of 1024 keys 18.5, most of it the way to
-// the first key (5 us) and from the last one through the exchange (6 us).  One token of 4 heads on 32 x 8 key heads of 777 to 8191
+// heads on 16 x 8 key heads of 512 to 4096 keys take 59 us (36 GFLOP), 44 rows on 32 heads of 1024 keys 17.8, most of it the way to
+// the first key (8 us) and from the last one through the exchange (5 us).  One token of 4 heads on 32 x 8 key heads of 777 to 8191
 // keys takes 41 us for 157 MB, 3.8 TB/s; while all workgroups are in their loops the cache streams at 5.2 to 5.7.  The smallest
 // call takes 7.7 us, a chain of trips to memory: lengths, queries, tree rows, prefix.
 #include <math.h>
@@ -1014,8 +1014,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
                     __syncthreads();
                     if ((int)*s_prev + 1 == n_pieces) {
                         if (tid == 0) __hip_atomic_store(p.ctr + (int64_t)first_piece * CTR_STRIDE, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                        // NF pieces at a time, everything of them requested at once; beyond the last one loads give zero
-                        constexpr int NF = C::PP >= 16 ? 2 : C::PP == 8 ? 4 : 8;
+                        // NF pieces at a time, everything of them requested at once; beyond the last one loads give zero.  As many as the
+                        // registers hold (64 rows: with 4 at a time 44 nodes on 32 heads of 1024 keys, five pieces, take 18.9 us, with 5
+                        // 17.9, with 6, which do not fit beside the rest, 20.8).
+                        constexpr int NF = C::PP >= 16 ? 2 : C::PP == 8 ? 5 : 8;
                         const auto off_of = [&](int i) { return (2 * i + (i == 0)) * ROWS; };
                         const auto rm = __builtin_amdgcn_make_buffer_rsrc((void *)(p.part_m + (int64_t)2 * first_piece * ROWS), 0, 2 * n_pieces * ROWS * 4, 0x00027000);
                         const auto rl = __builtin_amdgcn_make_buffer_rsrc((void *)(p.part_l + (int64_t)2 * first_piece * ROWS), 0, 2 * n_pieces * ROWS * 4, 0x00027000);

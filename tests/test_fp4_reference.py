@@ -3,6 +3,7 @@ a call that is refused launches nothing)."""
 import ctypes as C
 import math
 
+import numpy as np
 import pytest
 import torch
 
@@ -93,6 +94,18 @@ def test_attention_workspace_of_bad_shapes_is_zero():
         args = list(good)
         args[i] = bad
         assert b.tree_attention_fp4kv_workspace(*args) == 0, args
+
+
+def test_attention_workspace_serves_smaller_calls():
+    rng = np.random.default_rng(5)
+    for _ in range(400):
+        B, Hkv, g, d = (int(rng.choice(x)) for x in ((1, 2, 5, 16, 64, 200), (1, 2, 8, 32), (1, 3, 4, 8), (64, 128)))
+        n, prefix = int(rng.integers(1, 129)), int(rng.choice((0, 1, 64, 65, 500, 4096, 100000)))
+        row = int(rng.integers(0, n))
+        size = b.tree_attention_fp4kv_workspace(B, Hkv * g, Hkv, d, n, row, prefix)
+        fewer = int(rng.integers(1, n + 1))
+        rows, shorter = int(rng.integers(1, min(fewer, n - row) + 1)), int(rng.integers(0, prefix + 1))
+        assert b.tree_attention_fp4kv_workspace(B, Hkv * g, Hkv, d, fewer, fewer - rows, shorter) <= size
 
 
 def _store(dtype=1, B=2, H=4, d=128, rows=5, k=ONE, v=ONE, bs=4096, hs=128, rs=512, first=ONE, n=ONE, cache=CACHE, base=ONE, dst=128 * 128, cap=128):
