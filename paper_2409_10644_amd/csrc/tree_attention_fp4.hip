@@ -15,7 +15,7 @@
 //
 // Codes and scales stream from HBM straight into a ring of LDS stages.  The work is the tiles of all (sequence, head) pairs laid
 // end to end, the tree's own keys first in each, cut into pieces: equal ones of each pair where they fit the workgroups that are
-// resident at once, else equal pieces of the whole.  A pair's pieces leave their unnormalised output, maximum and sum in the
+// resident at once, else whole pairs, several to a workgroup, or equal pieces of the whole.  A pair's pieces leave their unnormalised output, maximum and sum in the
 // workspace, and the workgroup that is last to do so folds them.
 //
 // With more than 32 rows, blocks of 32 keys go through a pipeline: between the matrix instructions that make the scores of one and
@@ -118,7 +118,7 @@ struct Cfg {
     static constexpr int PP = CB * 4 / KG;           // pieces (four columns of a row per lane) that a wavefront ends up with
     static constexpr int XCHG = (KG - 1) * QBP * 32 * D * 4;
     static constexpr int LDS = RING + NV * VBUF > XCHG + 4 * 256 + 16 ? RING + NV * VBUF : XCHG + 4 * 256 + 16;
-    static_assert(LDS <= 80 * 1024, "two workgroups per compute unit");
+    static_assert(LDS + 64 * 13 <= 80 * 1024, "two workgroups per compute unit");
 };
 
 // V in LDS: 32 columns of all rows, 64 bytes each, then the next 32 columns (so that a transpose load takes the columns as an
@@ -306,6 +306,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     const Fp4AttnParams &p = args;
     using C = Cfg<D, QBP>;
     __shared__ __attribute__((aligned(1024))) unsigned char lds[C::LDS];
+    __shared__ int64_t s_base[64];                                     // of sequences b_lanes on: kept here while pairs are gone through
+    __shared__ int32_t s_len[64];
+    __shared__ unsigned char s_order[64];                              // by length, longest first
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
     const int qb = wave % QBP, kg = wave / QBP, w = blockIdx.x;
     const int tree_tiles = (p.n + C::T - 1) / C::T;
@@ -357,7 +360,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
             // nodes takes 62 us in pieces of 24 tiles and 70 in equal ones of 19; 32 of 777 to 8191 keys with a token each 48.5, 53.)
             const int t = len_l >= 0 ? tiles_of(len_l) : 0;
             auto fits = [&](int size) { return wave_last(wave_scan(small_div(t + size - 1, size))) * p.units <= resident; };
-            int lo = per, hi = per + per / 8 + (QBP == 1 ? 12 : 8);
+            int lo = per, hi = per + per / 8 + (QBP == 1 ? 12 : 8) * (1 + all);
             if (fits(hi)) {
                 while (lo < hi) {
                     const int mid = (lo + hi) >> 1;
@@ -369,6 +372,36 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         }
     }
     if (aligned) per = aligned;
+    // 4 times the place of the lane's sequence when they are in order of `size`, largest first (lanes without one stay where they are)
+    auto place_of = [&](int size) __attribute__((always_inline)) {
+        int rank = lane;
+        if (total < most * p.B && lane < p.B) {                        // (not all alike)
+            const unsigned key = (unsigned)size * 64 + 63 - lane;      // (fewer than 2^26 tiles)
+            rank = 0;
+#pragma unroll 4
+            for (int o = 0; o < p.B; ++o) rank += (unsigned)__builtin_amdgcn_readlane((int)key, o) > key;
+        }
+        return 4 * rank;
+    };
+    // Or whole pairs to every workgroup, the longest first, back and forth over the workgroups, where the fullest of them (of 64 looked
+    // at) has less to do than one with an equal piece, which begins and ends within pairs.  Equal pieces and whole pairs, us: 44 nodes
+    // on 64 x 32 heads of 100 to 2000 keys 266 and 134, on 20 x 20 of 10 to 3000 107 and 43; 60 nodes x 4 heads on 64 x 8 key heads of
+    // 100 to 2000 170 and 98, on 32 x 8 of 100 to 4000 158 and 98; one token on 64 x 32 heads of 100 to 2000 keys 176 and 95.
+    constexpr int BEGIN = 5, CROSS = QBP == 4 ? 24 : 16;               // tiles that a new pair costs, and one that is begun or ended within
+    const int pairs = p.B * p.units;
+    int rounds = 0;                                                    // > 0: of whole pairs
+    if (__builtin_expect(!aligned && p.B <= 64, 0)) {
+        const int t = len_l >= 0 ? tiles_of(len_l) : 0, place = place_of(t), sorted = __builtin_amdgcn_ds_permute(place, t);
+        s_order[lane] = (unsigned char)__builtin_amdgcn_ds_permute(place, lane);
+        const int n = (pairs + p.workgroups - 1) / p.workgroups, who = lane * (p.workgroups - 1) / 63;
+        int load = 0;
+        for (int k = 0; k < min(n, 32); ++k) {
+            const int at = k * p.workgroups + (k & 1 ? p.workgroups - 1 - who : who);
+            const int l = __builtin_amdgcn_ds_bpermute(4 * min(small_div(at, p.units), 63), sorted);
+            load += at < pairs ? l : 0;
+        }
+        if (n > 32 || wave_max(load) + BEGIN * n <= per + CROSS * (pairs / p.workgroups + 1)) rounds = n;
+    }
     int b = -1, unit = 0, tile = 0, n_pieces = 1, first_piece = 0, left = 0, number = w;
     {
         int before = 0, t = len_l >= 0 ? tiles_of(len_l) : 0, each = aligned ? small_div(t + per - 1, per) : t, seq = lane;
@@ -378,24 +411,25 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
             // units in turn, so the longest piece shares with the shortest: 41.9 us instead of 45.3 for 32 sequences of 777 to 8191
             // keys with a token each).
             const int pieces = wave_last(wave_scan(each * p.units));
-            if (pieces > p.single) {
-                const int size = each > 0 ? small_div(t + each - 1, each) : 0;
-                int rank = 0;
-                for (int o = 0; o < p.B; ++o) {
-                    const int other = __builtin_amdgcn_readlane(size, o);
-                    rank += other > size || (other == size && o < lane);
-                }
-                rank = 4 * (lane < p.B ? rank : lane);
-                t = __builtin_amdgcn_ds_permute(rank, t);
-                each = __builtin_amdgcn_ds_permute(rank, each);
-                seq = __builtin_amdgcn_ds_permute(rank, lane);
+            if (__builtin_expect(pieces > p.single, 0)) {
+                const int place = place_of(each > 0 ? small_div(t + each - 1, each) : 0);
+                t = __builtin_amdgcn_ds_permute(place, t);
+                each = __builtin_amdgcn_ds_permute(place, each);
+                seq = __builtin_amdgcn_ds_permute(place, lane);
                 if (w >= p.single) number = pieces - 1 - (w - p.single);
                 if (w >= p.single && number < p.single) return;
             }
         }
         const int here = aligned ? number : w * per;
+        if (__builtin_expect(rounds, 0)) {
+            if (w >= pairs) return;
+            const int l = uniform(small_div(w, p.units));
+            b = uniform(s_order[l]);
+            unit = w - l * p.units;
+            left = tiles_of(__builtin_amdgcn_readlane(len_l, b));
+        }
         for (int b0 = 0; b0 < p.B && b < 0; b0 += 64) {
-            if (p.B > 64) {
+            if (__builtin_expect(p.B > 64, 0)) {
                 if (b0 != b_lanes) fetch(b0);
                 t = len_l >= 0 ? tiles_of(len_l) : 0;
                 each = aligned ? small_div(t + per - 1, per) : t;      // per unit: splits, or tiles
@@ -422,6 +456,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         }
         if (b < 0) return;
     }
+    auto keep = [&]() __attribute__((always_inline)) {
+        s_len[lane] = len_l;                                           // (every wavefront writes the same, and reads what it wrote)
+        s_base[lane] = base_l;
+    };
+    keep();
+    int round = 0;
     int done = w * per;                                                // flat: tiles before this one
 
     // ---- what stays the same for all pairs ----
@@ -448,10 +488,14 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         constexpr int K_BLOCK = 32 / C::RW * C::WB;
         const int d_row = lane & 15, d_unit = lane >> 4;                   // the lane's quarter row when V is converted
         // ---- a piece of one pair: tiles [tile, tile + n) of sequence b, unit ----
-        if (b >= b_lanes + 64) fetch(b);
-        const int L = __builtin_amdgcn_readlane(len_l, b - b_lanes), all = tiles_of(L);
-        const int64_t seq_at = (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)((uint64_t)base_l >> 32), b - b_lanes) << 32 |
-                                         (uint32_t)__builtin_amdgcn_readlane((int)base_l, b - b_lanes));
+        if (__builtin_expect(b >= b_lanes + 64, 0)) {
+            __syncthreads();
+            fetch(b);
+            keep();
+        }
+        const int L = uniform(s_len[b - b_lanes]), all = tiles_of(L);
+        const int64_t s_at = s_base[b - b_lanes];
+        const int64_t seq_at = (int64_t)((uint64_t)(uint32_t)uniform((int)((uint64_t)s_at >> 32)) << 32 | (uint32_t)uniform((int)s_at));
         const int n = min(left, all - tile), end = tile + n;
         const int kvh = row_div(unit, p.by_chunks), chunk = unit - kvh * p.chunks;
         const int64_t pre = seq_at + kvh * p.head_stride, tree = ((int64_t)b * p.H_kv + kvh) * p.node_stride * D;
@@ -1062,6 +1106,16 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         left -= n;
         tile = 0;
         if (aligned) break;
+        if (rounds) {
+            if (++round == rounds) break;
+            const int at = round * p.workgroups + (round & 1 ? p.workgroups - 1 - w : w);
+            if (at >= pairs) break;
+            const int l = uniform(small_div(at, p.units));
+            b = uniform(s_order[l]);
+            unit = at - l * p.units;
+            left = tiles_of(uniform(s_len[b]));
+            continue;
+        }
         if (++unit == p.units) {
             unit = 0;
             if (++b == p.B) break;

@@ -114,6 +114,21 @@ def test_ragged_batches(binding, d, B, Hq, Hkv, tree, lo, hi):
     assert torch.equal(c.run(), first)                     # the same call gives the same bits
 
 
+@pytest.mark.parametrize("B,Hq,Hkv,d,tree,lo,hi", [(64, 32, 32, 64, "one", 0, 700), (20, 32, 32, 128, "44", 0, 900), (48, 24, 12, 128, "120", 1, 400), (61, 40, 40, 64, "nine", 0, 200),
+                                                     (64, 9, 9, 128, "one", 7, 7), (40, 26, 13, 64, "120", 0, 1500)])
+def test_more_pairs_than_workgroups(binding, B, Hq, Hkv, d, tree, lo, hi):
+    """Several whole pairs to a workgroup, or pieces that cross them: every pair is written, a sample of them compared."""
+    gen = torch.Generator().manual_seed(B * d)
+    lens = torch.randint(lo, hi + 1, (B,), generator=gen).tolist()
+    lens[1], lens[-1] = lo, hi
+    c = Call(binding, TREES[tree], B, Hq, Hkv, d, lens, seed=B)
+    pairs = {(int(b), int(h)) for b, h in zip(torch.randint(0, B, (40,), generator=gen), torch.randint(0, Hq, (40,), generator=gen))}
+    out = c.check(pairs | {(0, 0), (1, Hq - 1), (B - 1, 0), (B - 1, Hq - 1)})
+    assert bool(torch.isfinite(out[:, :, :c.n].float()).all()) and not bool((out[:, :, :c.n] == 31).all(-1).any())
+    again = c.run()
+    assert torch.equal(out, again)
+
+
 def test_a_serving_batch_of_conversations(binding):
     lens = [512 + (3584 * i) // 15 for i in range(16)][::-1]
     Call(binding, (4, 2, 2, 2), 16, 32, 8, 128, lens, seed=4).check({(b, h) for b in range(16) for h in (b, 31 - b)})
