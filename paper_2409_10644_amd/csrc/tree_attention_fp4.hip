@@ -75,6 +75,7 @@ constexpr uint32_t WS_TAG = 0x4d435344u;
 constexpr size_t WS_HEADER = 256, WS_CTR_BYTES = 64 * 1024;
 constexpr int CTR_STRIDE = 16;                       // a counter per 128-byte line: atomics on one line queue
 constexpr int MAX_PIECES = (int)(WS_CTR_BYTES / 8 / CTR_STRIDE);
+constexpr int KEPT = 256;                            // sequences whose lengths a workgroup keeps, one per thread
 constexpr int MAX_SPLITS = 32;                       // pieces of one (sequence, head): one workgroup folds them
 
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -118,7 +119,7 @@ struct Cfg {
     static constexpr int PP = CB * 4 / KG;           // pieces (four columns of a row per lane) that a wavefront ends up with
     static constexpr int XCHG = (KG - 1) * QBP * 32 * D * 4;
     static constexpr int LDS = RING + NV * VBUF > XCHG + 4 * 256 + 16 ? RING + NV * VBUF : XCHG + 4 * 256 + 16;
-    static_assert(LDS + 64 * 13 <= 80 * 1024, "two workgroups per compute unit");
+    static_assert(LDS + KEPT * 13 <= 80 * 1024, "two workgroups per compute unit");
 };
 
 // V in LDS: 32 columns of all rows, 64 bytes each, then the next 32 columns (so that a transpose load takes the columns as an
@@ -306,9 +307,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     const Fp4AttnParams &p = args;
     using C = Cfg<D, QBP>;
     __shared__ __attribute__((aligned(1024))) unsigned char lds[C::LDS];
-    __shared__ int64_t s_base[64];                                     // of sequences b_lanes on: kept here while pairs are gone through
-    __shared__ int32_t s_len[64];
-    __shared__ unsigned char s_order[64];                              // by length, longest first
+    __shared__ int64_t s_base[KEPT];                                   // of sequences `kept` on (all of up to KEPT): here while pairs are gone through
+    __shared__ int32_t s_len[KEPT];
+    __shared__ unsigned char s_order[KEPT];                            // by length, longest first
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
     const int qb = wave % QBP, kg = wave / QBP, w = blockIdx.x;
     const int tree_tiles = (p.n + C::T - 1) / C::T;
@@ -329,8 +330,14 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     fetch(0);
     const bool prepared = p.ws_tag && uniform((int)*p.ws_tag) == (int)WS_TAG;
     int total = 0, most = 0;                                           // tiles of one unit of every sequence
+    int kept = 0;
+    auto keep = [&](int at) __attribute__((always_inline)) {           // (every wavefront writes the same, and reads what it wrote)
+        s_len[at + lane] = len_l;
+        s_base[at + lane] = base_l;
+    };
     for (int b0 = 0; b0 < p.B; b0 += 64) {
         if (b0) fetch(b0);
+        if (p.B <= KEPT) keep(b0);                                     // (with more of them only the ones at hand, below)
         const int t = len_l >= 0 ? tiles_of(len_l) : 0;
         total += wave_last(wave_scan(t));
         most = max(most, wave_max(t));
@@ -386,19 +393,30 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     // Or whole pairs to every workgroup, the longest first, back and forth over the workgroups, where the fullest of them (of 64 looked
     // at) has less to do than one with an equal piece, which begins and ends within pairs.  Equal pieces and whole pairs, us: 44 nodes
     // on 64 x 32 heads of 100 to 2000 keys 266 and 134, on 20 x 20 of 10 to 3000 107 and 43; 60 nodes x 4 heads on 64 x 8 key heads of
-    // 100 to 2000 170 and 98, on 32 x 8 of 100 to 4000 158 and 98; one token on 64 x 32 heads of 100 to 2000 keys 176 and 95.
+    // 100 to 2000 170 and 98, on 32 x 8 of 100 to 4000 158 and 98; one token on 64 x 32 heads of 100 to 2000 keys 176 and 95, of 4
+    // heads on 128 x 8 key heads of 100 to 4000 124 and 79.
     constexpr int BEGIN = 5, CROSS = QBP == 4 ? 24 : 16;               // tiles that a new pair costs, and one that is begun or ended within
     const int pairs = p.B * p.units;
     int rounds = 0;                                                    // > 0: of whole pairs
-    if (__builtin_expect(!aligned && p.B <= 64, 0)) {
-        const int t = len_l >= 0 ? tiles_of(len_l) : 0, place = place_of(t), sorted = __builtin_amdgcn_ds_permute(place, t);
-        s_order[lane] = (unsigned char)__builtin_amdgcn_ds_permute(place, lane);
+    if (__builtin_expect(!aligned && p.B <= KEPT, 0)) {
+        int rank = tid;
+        if (total < most * p.B && tid < p.B) {                         // (not all alike)
+            const int own = s_len[tid];
+            rank = 0;
+#pragma unroll 8
+            for (int o = 0; o < p.B; ++o) {
+                const int other = s_len[o];
+                rank += other > own || (other == own && o < tid);
+            }
+        }
+        s_order[rank] = (unsigned char)tid;
+        __syncthreads();
         const int n = (pairs + p.workgroups - 1) / p.workgroups, who = lane * (p.workgroups - 1) / 63;
         int load = 0;
         for (int k = 0; k < min(n, 32); ++k) {
             const int at = k * p.workgroups + (k & 1 ? p.workgroups - 1 - who : who);
-            const int l = __builtin_amdgcn_ds_bpermute(4 * min(small_div(at, p.units), 63), sorted);
-            load += at < pairs ? l : 0;
+            const int t = tiles_of(s_len[s_order[min(small_div(at, p.units), p.B - 1)]]);
+            load += at < pairs ? t : 0;
         }
         if (n > 32 || wave_max(load) + BEGIN * n <= per + CROSS * (pairs / p.workgroups + 1)) rounds = n;
     }
@@ -426,7 +444,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
             const int l = uniform(small_div(w, p.units));
             b = uniform(s_order[l]);
             unit = w - l * p.units;
-            left = tiles_of(__builtin_amdgcn_readlane(len_l, b));
+            left = tiles_of(uniform(s_len[b]));
         }
         for (int b0 = 0; b0 < p.B && b < 0; b0 += 64) {
             if (__builtin_expect(p.B > 64, 0)) {
@@ -456,11 +474,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         }
         if (b < 0) return;
     }
-    auto keep = [&]() __attribute__((always_inline)) {
-        s_len[lane] = len_l;                                           // (every wavefront writes the same, and reads what it wrote)
-        s_base[lane] = base_l;
-    };
-    keep();
+    if (__builtin_expect(p.B > KEPT, 0)) {
+        kept = b_lanes;
+        keep(0);
+    }
     int round = 0;
     int done = w * per;                                                // flat: tiles before this one
 
@@ -488,13 +505,14 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         constexpr int K_BLOCK = 32 / C::RW * C::WB;
         const int d_row = lane & 15, d_unit = lane >> 4;                   // the lane's quarter row when V is converted
         // ---- a piece of one pair: tiles [tile, tile + n) of sequence b, unit ----
-        if (__builtin_expect(b >= b_lanes + 64, 0)) {
+        if (__builtin_expect(p.B > KEPT && b >= kept + 64, 0)) {
             __syncthreads();
+            kept = b;
             fetch(b);
-            keep();
+            keep(0);
         }
-        const int L = uniform(s_len[b - b_lanes]), all = tiles_of(L);
-        const int64_t s_at = s_base[b - b_lanes];
+        const int L = uniform(s_len[b - kept]), all = tiles_of(L);
+        const int64_t s_at = s_base[b - kept];
         const int64_t seq_at = (int64_t)((uint64_t)(uint32_t)uniform((int)((uint64_t)s_at >> 32)) << 32 | (uint32_t)uniform((int)s_at));
         const int n = min(left, all - tile), end = tile + n;
         const int kvh = row_div(unit, p.by_chunks), chunk = unit - kvh * p.chunks;

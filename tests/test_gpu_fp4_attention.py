@@ -115,7 +115,8 @@ def test_ragged_batches(binding, d, B, Hq, Hkv, tree, lo, hi):
 
 
 @pytest.mark.parametrize("B,Hq,Hkv,d,tree,lo,hi", [(64, 32, 32, 64, "one", 0, 700), (20, 32, 32, 128, "44", 0, 900), (48, 24, 12, 128, "120", 1, 400), (61, 40, 40, 64, "nine", 0, 200),
-                                                     (64, 9, 9, 128, "one", 7, 7), (40, 26, 13, 64, "120", 0, 1500)])
+                                                     (64, 9, 9, 128, "one", 7, 7), (40, 26, 13, 64, "120", 0, 1500),
+                                                     (100, 16, 8, 128, "one", 0, 1200), (256, 6, 6, 64, "nine", 0, 150), (300, 8, 2, 64, "one", 0, 500), (257, 1, 1, 128, "44", 100, 130)])
 def test_more_pairs_than_workgroups(binding, B, Hq, Hkv, d, tree, lo, hi):
     """Several whole pairs to a workgroup, or pieces that cross them: every pair is written, a sample of them compared."""
     gen = torch.Generator().manual_seed(B * d)
