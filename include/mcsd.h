@@ -428,7 +428,8 @@ int mcsd_tree_attention_fp4kv(const mcsd_mask_view_t *mask, int32_t B, int32_t H
  * first_row_dev, n_rows_dev : DEVICE int32 [B]; n_rows is clamped to 0..max_rows; rows of the cache outside 0..capacity-1
  *           are skipped, never touched
  * capacity: rows every (sequence, head) of the cache can hold
- * Limits: d 64 or 128; max_rows * H < 2^31.  max_rows == 0 does nothing.  One launch, no workspace. */
+ * Limits: d 64 or 128; max_rows * H <= 2^28 - 16 (d 128) or 2^29 - 32 (d 64), the lanes of a launch.  max_rows == 0 does
+ * nothing.  One launch, no workspace. */
 int mcsd_store_fp4kv(mcsd_dtype_t dtype, int32_t B, int32_t H, int32_t d, int32_t max_rows, const void *k, const void *v,
                      int64_t batch_stride, int64_t src_head_stride, int64_t row_stride, const int32_t *first_row_dev,
                      const int32_t *n_rows_dev, const mcsd_fp4_cache_t *cache, const int64_t *seq_base_dev,

@@ -125,7 +125,7 @@ int check_rows(mcsd_dtype_t dtype, int32_t B, int32_t H, int32_t d, int32_t max_
     if (((batch_stride | other_head_stride | row_stride) & 7) || (head_stride & 127)) return MCSD_EINVAL;
     if (d != 64 && d != 128) return MCSD_EUNSUPPORTED;
     const int64_t rows = (int64_t)max_rows * H, per_wg = 256 / (d / 8);
-    if (rows > 0x7fffffff - per_wg) return MCSD_EUNSUPPORTED;
+    if ((rows + per_wg - 1) / per_wg > MCSD_MAX_GRID_256) return MCSD_EUNSUPPORTED;
     grid_x = (unsigned)((rows + per_wg - 1) / per_wg);
     return MCSD_OK;
 }

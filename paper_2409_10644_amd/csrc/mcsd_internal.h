@@ -27,6 +27,9 @@ struct McsdTreeDesc {
     int32_t off[MCSD_MAX_LEVELS + 1];
 };
 
+// Workgroups of 256 lanes that one direction of a launch can have: its lanes are counted in 32 bits.
+constexpr int64_t MCSD_MAX_GRID_256 = 0xffffff;
+
 static inline int mcsd_hip_status(hipError_t e) { return e == hipSuccess ? MCSD_OK : MCSD_EHIP; }
 
 // Accelerator dies (each with its own L2) of `device` when the hardware deals workgroup i of a launch to die
