@@ -474,7 +474,8 @@ int mcsd_commit_path_fp4kv(const mcsd_mask_view_t *mask, int32_t B, int32_t H, i
  *                 neither (NULL).
  * rope          : HOST struct; inv_freq DEVICE fp32 [rotary_dim/2] (radians per position), q_weight and k_weight DEVICE fp32 [d]
  *                 or NULL, eps >= 0 and finite, rotary_dim a multiple of 16 in 0..d (0: no rotation, inv_freq not read)
- * Limits: d 64 or 128; 16-byte aligned tensors, strides >= 0 and multiples of 8 elements; (H_q + 2 H_kv) <= 65535.
+ * Limits: d 64 or 128; 16-byte aligned tensors, strides >= 0 and multiples of 8 elements; (H_q + 2 H_kv) <= 65535;
+ * max_rows <= 2^26 - 4.
  * One launch, no workspace.
  * ------------------------------------------------------------------------------------------------- */
 typedef struct mcsd_rope {

@@ -181,7 +181,7 @@ int qk_call(const mcsd_mask_view_t *mask, mcsd_dtype_t dtype, int32_t B, int32_t
     if (!(rope->eps >= 0.f) || rope->eps > 3.4e38f || rope->rotary_dim < 0 || rope->rotary_dim > d || (rope->rotary_dim & 15)) return MCSD_EINVAL;
     if (rope->rotary_dim > 0 && !rope->inv_freq) return MCSD_EINVAL;
     if (d != 64 && d != 128) return MCSD_EUNSUPPORTED;
-    if ((int64_t)H_q + 2 * (int64_t)H_kv > 65535) return MCSD_EUNSUPPORTED;
+    if ((int64_t)H_q + 2 * (int64_t)H_kv > 65535 || rows > 4 * MCSD_MAX_GRID_256) return MCSD_EUNSUPPORTED;
     if (rows == 0) return MCSD_OK;
 
     QkParams p = {};
@@ -199,8 +199,8 @@ int qk_call(const mcsd_mask_view_t *mask, mcsd_dtype_t dtype, int32_t B, int32_t
     p.by_heads = row_div_of((uint32_t)p.heads);
     // Four rows per workgroup where one leaves lanes idle (64000 rows of 12 heads: 73 us, one by one 101; 8000 of 12: 11.0, 13.3),
     // unless there are so few that the workgroups count (2000 rows of 12: 5.5, one by one 4.9).  With whole rows of lanes one by
-    // one is the faster (5000 rows of 48 heads: 27.0 us, four at a time 28.9; 44 of 96: 4.3, 9.4).
-    if (p.heads * (d / 16) < 256 && (int64_t)rows * B > 2048) launch<4>(p, d, dtype == MCSD_F32, B, (hipStream_t)hip_stream);
+    // one is the faster (5000 rows of 48 heads: 27.0 us, four at a time 28.9; 44 of 96: 4.3, 9.4), as long as one launch holds them.
+    if ((p.heads * (d / 16) < 256 && (int64_t)rows * B > 2048) || rows > MCSD_MAX_GRID_256) launch<4>(p, d, dtype == MCSD_F32, B, (hipStream_t)hip_stream);
     else launch<1>(p, d, dtype == MCSD_F32, B, (hipStream_t)hip_stream);
     return mcsd_hip_status(hipGetLastError());
 }
