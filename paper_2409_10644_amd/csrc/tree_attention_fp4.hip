@@ -313,7 +313,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
     const int qb = wave % QBP, kg = wave / QBP, w = blockIdx.x;
     const int tree_tiles = (p.n + C::T - 1) / C::T;
-    auto tiles_of = [&](int len) { return tree_tiles + (int)((unsigned)(len + C::T - 1) / C::T); };
+    auto tiles_of = [&](int len) { return tree_tiles + (int)(((unsigned)len + C::T - 1) / C::T); };
 
     // ---- this workgroup's piece of the work: `left` tiles of the whole from tile `tile` of (b, unit) on, or a split of one pair ----
     // Lengths and bases of 64 sequences from b_lanes on, one per lane (in most calls those of all: one trip to memory).
@@ -894,7 +894,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
             };
             constexpr std::true_type YES;
             constexpr std::false_type NO;
-            const int valid0 = min(L, t1 * C::T) - t0 * C::T;          // keys of the piece
+            const int valid0 = min(L - t0 * C::T, n_pre * C::T);       // keys of the piece (the end of the last tile may be 2^31)
             // a tile's own slot is over: its V is converted everywhere, its stage free, and tile `need` has arrived everywhere
             constexpr int NEED = 3 - C::U;                             // tile x + NEED
             // Of two workgroups on a compute unit the older one would always go first, and the other be alone at the end, at half

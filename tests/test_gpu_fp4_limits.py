@@ -1,5 +1,7 @@
 """The largest bounds that the entry points around the 4-bit cache document, with few rows that exist: the launch is as large as it
 gets, and all but a few of its workgroups find nothing to do."""
+import math
+
 import pytest
 import torch
 
@@ -52,3 +54,33 @@ def test_prompt_rows_up_to_a_launch(binding, d, most):
         # fp32: half a step of the output, and fewer than 32 roundings on the way (angle, sine, products)
         assert bool(((out[:n].double() - want).abs() <= 2.0 ** -24 * want.abs() + 32 * 2.0 ** -24 * size).all())
         assert bool((out[n:] == 7).all())
+
+
+@pytest.mark.parametrize("branching", [(2,), (4, 2, 2, 1), (8, 2, 2, 1, 1)])
+def test_the_longest_prefix(binding, branching):
+    """2^31 - 1 keys of one head, 68 GiB of codes and scales that keys and values share.  All numbers are 1 but those of the last 63
+    rows, which are 6 and draw most of the weight: a row that misses them, or some of them, is far off."""
+    d, L, tail, g = 64, 2 ** 31 - 1, 63, len(branching)
+    codes = torch.full((L + 1, d // 2), 0x22, dtype=torch.uint8, device="cuda")
+    codes[L - tail:] = 0x77
+    scales = torch.full((L + 1, d // 32), 127, dtype=torch.uint8, device="cuda")
+    view = binding.slice_mask(binding.build_mask(branching), g)
+    n, scale = view.n_nodes, 0.125
+    q = torch.full((1, 1, n, d), 0.5, dtype=torch.bfloat16, device="cuda")
+    kt, vt, out = torch.zeros_like(q), torch.zeros_like(q), torch.zeros_like(q)
+    size = binding.tree_attention_fp4kv_workspace(1, 1, 1, d, n, 0, L)
+    binding.tree_attention_fp4kv(view, 1, 1, 1, d, 0, q, kt, vt, n, binding.make_fp4_cache(codes, scales, codes, scales), torch.zeros(1, dtype=torch.int64, device="cuda"),
+                                 _i32(L), 0, L, scale, out, binding.new_workspace(size))
+    torch.cuda.synchronize()
+    got = out.double()
+    del codes, scales
+    torch.cuda.empty_cache()
+    # scores 4 and 24, of the tree's own keys 0 (their values are 0; a node sees at most g of them)
+    ones, sixes = (L - tail) * math.exp(4.0 - 24.0), float(tail)
+    want = (ones + 6 * sixes) / (ones + sixes)
+    # output and weights rounded to bf16 (2^-8 each); a score off by scale * 2^-12 / 3.75 * max|q| * sum|k| (two groups of 32) and by
+    # 160 roundings of fp32 of its size; the sums: parts of 2^26 equal weights at most, added 16 at a time and so exact up to 2^28,
+    # and 32 parts of 2^-24; the tree's weights
+    delta = scale * 2.0 ** -12 / 3.75 * 0.5 * d * 6 + 160 * 2.0 ** -24 * 24
+    lim = want * (2 * 2.0 ** -8 + math.expm1(2 * delta) + 64 * 2.0 ** -24 + g * math.exp(-4.0) / L)
+    assert abs(want - 1) > 10 * lim and bool(((got - want).abs() <= lim).all()), (want, lim, got.min().item(), got.max().item())
