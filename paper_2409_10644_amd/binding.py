@@ -519,13 +519,22 @@ def make_rope(rotary_dim: int, inv_freq: Optional[torch.Tensor], q_weight: Optio
         raise McsdError(MCSD_EINVAL, "make_rope (a frequency for every pair)")
     r = Rope(int(rotary_dim), int(bool(interleaved)), float(eps), _ptr(inv_freq), _ptr(q_weight), _ptr(k_weight))
     r._keep = (inv_freq, q_weight, k_weight)      # the struct holds raw pointers
+    r._weights = min((w.numel() for w in (q_weight, k_weight) if w is not None), default=None)      # the shorter one's numbers
     return r
+
+
+def _weights_of(rope: Rope, d: int, where: str) -> None:
+    """Norm weights have a number for each of d channels: the kernel reads as many."""
+    n = getattr(rope, "_weights", None)
+    if n is not None and n < d:
+        raise McsdError(MCSD_EINVAL, f"{where} (norm weights of fewer than {d} numbers)")
 
 
 def tree_qk_norm_rope(view: MaskView, dtype: int, B: int, H_q: int, H_kv: int, d: int, row_begin: int, q_in: torch.Tensor,
                       k_in: torch.Tensor, v_in: Optional[torch.Tensor], q_batch_stride: int, q_row_stride: int, kv_batch_stride: int,
                       kv_row_stride: int, rope: Rope, prefix_lens_dev: torch.Tensor, max_prefix: int, q_out: torch.Tensor,
                       k_out: torch.Tensor, v_out: Optional[torch.Tensor], node_stride: int, stream=None) -> None:
+    _weights_of(rope, d, "mcsd_tree_qk_norm_rope")
     _pycall.tree_qk_norm_rope(view, dtype, B, H_q, H_kv, d, row_begin, q_in, k_in, v_in, q_batch_stride, q_row_stride, kv_batch_stride,
                               kv_row_stride, rope, prefix_lens_dev, max_prefix, q_out, k_out, v_out, node_stride, stream)
 
@@ -534,6 +543,7 @@ def prompt_qk_norm_rope(dtype: int, B: int, H_q: int, H_kv: int, d: int, max_row
                         v_in: Optional[torch.Tensor], q_batch_stride: int, q_row_stride: int, kv_batch_stride: int, kv_row_stride: int,
                         rope: Rope, first_pos_dev: torch.Tensor, n_rows_dev: torch.Tensor, q_out: torch.Tensor, k_out: torch.Tensor,
                         v_out: Optional[torch.Tensor], out_row_stride: int, stream=None) -> None:
+    _weights_of(rope, d, "mcsd_prompt_qk_norm_rope")
     _pycall.prompt_qk_norm_rope(dtype, B, H_q, H_kv, d, max_rows, q_in, k_in, v_in, q_batch_stride, q_row_stride, kv_batch_stride,
                                 kv_row_stride, rope, first_pos_dev, n_rows_dev, q_out, k_out, v_out, out_row_stride, stream)
 

@@ -1,9 +1,10 @@
 """The largest calls that the entry points around the 4-bit cache document, and the refusal of the next larger ones (no GPU needed:
 a call that is refused launches nothing)."""
 import pytest
+import torch
 
 from paper_2409_10644_amd import binding as b
-from test_fp4_reference import _load, _qk, _store
+from test_fp4_reference import NoStream, _load, _qk, _store, _view
 
 LANES = 2 ** 32                                            # of a launch, in one direction: fewer than that
 
@@ -25,3 +26,16 @@ def test_prompts_beyond_a_launch_are_refused(Hq, Hkv):
     most = 4 * (LANES // 256 - 1)
     for rows in (most + 1, 2 ** 31 - 1):
         assert _qk(False, Hq=Hq, Hkv=Hkv, rows=rows, out=rows) == b.MCSD_EUNSUPPORTED, rows
+
+
+@pytest.mark.parametrize("short", ["q", "k", "both"])
+def test_norm_weights_shorter_than_a_head_are_refused(short):
+    """The kernel reads a weight per channel: 64 of them do not serve heads of 128."""
+    t, weight = torch.zeros(128), torch.ones(64)
+    rope = b.make_rope(64, torch.zeros(32), t if short == "k" else weight, t if short == "q" else weight)
+    view = _view()
+    for call in (lambda: b.tree_qk_norm_rope(view, 0, 1, 1, 1, 128, 0, t, t, None, 0, 0, 0, 0, rope, t, 8, t, t, None, 44, NoStream),
+                 lambda: b.prompt_qk_norm_rope(0, 1, 1, 1, 128, 1, t, t, None, 0, 0, 0, 0, rope, t, t, t, t, None, 44, NoStream)):
+        with pytest.raises(b.McsdError) as e:
+            call()
+        assert e.value.status == b.MCSD_EINVAL
