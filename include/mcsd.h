@@ -402,10 +402,14 @@ typedef struct mcsd_fp4_cache {
 /* Tree attention over such a prefix cache: as mcsd_tree_attention_gqa with dtype MCSD_BF16 (q, k_tree, v_tree and out are
  * bf16; d 64 or 128), except that the prefix rows are those of *cache (HOST struct).  The query rows of the query heads that
  * share a key/value head are served together, up to 128 per workgroup, whichever heads they belong to.
- * Precision: scores of prefix keys are exact to about 2^-13 of |q| |k| before the soft-max scale: a query, times the scale
- * and log2 e, enters the matrix unit as three 6-bit terms per 32 channels that leave 2^-14 of the group's largest magnitude.
- * Weights are rounded to bf16 for the product with the values (the denominator is summed in fp32); partial results of split
- * keys are exchanged in fp32.
+ * Precision: a query, times the scale and log2 e, meets the prefix keys as three 6-bit terms per group of 32 channels, which
+ * leave of each channel at most e = 2^-12 / 3.75 of the group's largest magnitude.  So a prefix key's score, before the soft-max
+ * scale, is off by at most the sum over groups of e max|q| sum|k|, which is at most 3.02 * 2^-13 of |q| |k| (sqrt(32) e), beside
+ * roundings of fp32.  Channels below about a thirtieth of their group's largest keep fewer bits than bf16 gave them; where a
+ * query's small channels matter beside one that is hundreds of times larger, mcsd_tree_attention_gqa and
+ * mcsd_tree_attention_fp8kv multiply bf16 queries as they are.  Scores of the tree's own keys are products of the bf16 numbers.
+ * Weights are rounded to bf16 for the product with the values, as in those calls (the denominator is summed in fp32 from the
+ * weights before that); partial results of split keys are exchanged in fp32.
  * workspace : DEVICE, mcsd_tree_attention_fp4kv_workspace(...) bytes (0: may be NULL), 256-byte aligned, prepared with
  *             mcsd_workspace_init; the rules of mcsd_tree_attention hold.  The size for a call serves calls of the same B, H_q,
  *             H_kv and d with fewer nodes, rows or prefix keys.
