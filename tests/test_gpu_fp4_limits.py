@@ -7,6 +7,7 @@ import torch
 
 import fp4_reference as R
 from fp4_reference import Cache
+from test_gpu_fp4_attention import Call
 
 pytestmark = pytest.mark.gpu
 
@@ -86,3 +87,17 @@ def test_the_longest_prefix(binding, branching, L, tail):
     delta = scale * 2.0 ** -12 / 3.75 * 0.5 * d * 6 + 160 * 2.0 ** -24 * 24
     lim = want * (2 * 2.0 ** -8 + math.expm1(2 * delta) + 64 * 2.0 ** -24 + g * math.exp(-4.0) / L)
     assert abs(want - 1) > 10 * lim and abs(want - 6) > lim and bool(((got - want).abs() <= lim).all()), (want, lim, got.min().item(), got.max().item())
+
+
+@pytest.mark.parametrize("B,H,hi", [(256, 80, 100), (1000, 1, 900), (700, 3, 40)])
+def test_many_sequences_and_heads(binding, B, H, hi):
+    """More than 32 whole pairs to a workgroup; and more sequences than a workgroup keeps the lengths of."""
+    gen = torch.Generator().manual_seed(B)
+    lens = torch.randint(0, hi + 1, (B,), generator=gen).tolist()
+    lens[0], lens[-1] = hi, 0
+    c = Call(binding, (2,), B, H, H, 64, lens, seed=B)
+    pairs = {(int(b), int(h)) for b, h in zip(torch.randint(0, B, (60,), generator=gen), torch.randint(0, H, (60,), generator=gen))}
+    out = c.check(pairs | {(0, 0), (B - 1, H - 1), (B // 2, 0), (256 % B, 0), (255, H - 1)})
+    assert not bool((out[:, :, :c.n] == 31).all(-1).any())                       # every pair is written
+    c.out.fill_(31)
+    assert torch.equal(c.run(), out)
