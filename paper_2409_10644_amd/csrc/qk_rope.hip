@@ -5,7 +5,7 @@
 // pieces of eight: the pieces are chosen so that a lane holds both ends of the pairs it rotates, and the sum of squares takes two
 // or three exchanges between neighbouring lanes.  The sines and cosines of a row serve all its heads: they are computed once per
 // workgroup, one angle per lane, and shared through LDS.  Angles are products in binary64, reduced to a fraction of a turn there,
-// so position 10^6 is as exact as position 1.
+// so position 10^6 is as exact as position 1.  Squares are summed in fp32, of a scaled vector where its size asks for it.
 //
 // Bound by memory: prompts of 500 to 2000 tokens of 48 heads of 128 channels in bf16 (123 MB read and written) take 26 to 28 us,
 // 4.4 to 4.7 TB/s where a large copy runs at 4.9; the 44 tree nodes of one sequence take 4.3 us, a launch and two trips to memory.
@@ -118,13 +118,29 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(const QkParams p)
             const float *w = is_q ? p.wq : p.wk;
             if (w) {
                 const float *sw = s_w[is_q ? 0 : 1];
-                float ss = 0.f;
+                const auto mean_square = [&]() __attribute__((always_inline)) {
+                    float ss = 0.f;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) ss = fmaf(x[j], x[j], fmaf(y[j], y[j], ss));
-                ss += __uint_as_float(dpp_move<DPP_XOR1>(__float_as_uint(ss)));
-                ss += __uint_as_float(dpp_move<DPP_XOR2>(__float_as_uint(ss)));
-                if (LANES == 8) ss += __uint_as_float(dpp_move<DPP_HALF_MIRROR>(__float_as_uint(ss)));
-                const float inv = 1.f / sqrtf(ss * (1.f / D) + p.eps);
+                    for (int j = 0; j < 8; ++j) ss = fmaf(x[j], x[j], fmaf(y[j], y[j], ss));
+                    ss += __uint_as_float(dpp_move<DPP_XOR1>(__float_as_uint(ss)));
+                    ss += __uint_as_float(dpp_move<DPP_XOR2>(__float_as_uint(ss)));
+                    if (LANES == 8) ss += __uint_as_float(dpp_move<DPP_HALF_MIRROR>(__float_as_uint(ss)));
+                    return ss * (1.f / D);
+                };
+                float mean = mean_square() + p.eps;
+                // Beyond fp32, or so small that squares were below it: the same of the vector times 2^-68 (128 squares of the largest
+                // number are below 2^128 then) or 2^100, which the norm takes out again.  (The condition is that of all the vector's
+                // lanes.)
+                if (__builtin_expect(!(mean >= 0x1p-100f && mean < INFINITY), 0)) {
+                    const float by = mean < 1.f ? 0x1p100f : 0x1p-68f;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        x[j] *= by;
+                        y[j] *= by;
+                    }
+                    mean = mean_square() + p.eps * by * by;
+                }
+                const float inv = 1.f / sqrtf(mean);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     x[j] = x[j] * inv * sw[pa * 8 + j];
