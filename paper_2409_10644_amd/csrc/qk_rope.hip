@@ -147,23 +147,23 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(const QkParams p)
                     y[j] = y[j] * inv * sw[pb * 8 + j];
                 }
             }
-            if (c < pairs) {
+            if (c < pairs) {                                           // (which product is rounded first is written out: every build gives the same bits)
                 if (!p.interleaved) {
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
                         const float co = s_cos[row][pa * 8 + j], si = s_sin[row][pa * 8 + j], u = x[j], v = y[j];
-                        x[j] = u * co - v * si;
-                        y[j] = v * co + u * si;
+                        x[j] = fmaf(u, co, -(v * si));
+                        y[j] = fmaf(v, co, u * si);
                     }
                 } else {
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         float co = s_cos[row][pa * 4 + j], si = s_sin[row][pa * 4 + j], u = x[2 * j], v = x[2 * j + 1];
-                        x[2 * j] = u * co - v * si;
-                        x[2 * j + 1] = v * co + u * si;
+                        x[2 * j] = fmaf(u, co, -(v * si));
+                        x[2 * j + 1] = fmaf(v, co, u * si);
                         co = s_cos[row][pb * 4 + j], si = s_sin[row][pb * 4 + j], u = y[2 * j], v = y[2 * j + 1];
-                        y[2 * j] = u * co - v * si;
-                        y[2 * j + 1] = v * co + u * si;
+                        y[2 * j] = fmaf(u, co, -(v * si));
+                        y[2 * j + 1] = fmaf(v, co, u * si);
                     }
                 }
             }
