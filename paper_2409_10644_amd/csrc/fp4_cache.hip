@@ -5,8 +5,9 @@
 // maximum needs two exchanges within the quad; consecutive rows of a workgroup are consecutive tokens of one head, whose codes
 // and scales are neighbours in the cache while each of them is whole lines of the source.
 //
-// Bound by memory: 147200 rows of 128 channels stored take 21 to 24 us and loaded 16.6 us (95 MB each: 4.2 and 5.7 TB/s, a large
-// copy runs at 4.9); one row for each of 16 sequences takes 2.5 us either way, a launch.  One row per lane: with two, all requested
+// Bound by memory: 147200 rows of 128 channels stored take 18 to 24 us and loaded 16.6 to 20, by what the last-level cache holds of
+// them (95 MB each: 4 to 5.7 TB/s, a large copy runs at 4.9), in fp32 34 and 38 us (171 MB); one row for each of 16 sequences takes
+// 2.4 us either way, a launch.  One row per lane: with two, all requested
 // before the first is used, the pair of calls takes 44.8 us instead of 43.1 there and 5.2 instead of 4.8 for 16 sequences of 16
 // rows; with four 48.2 and 7.1.  Eight wavefronts per SIMD hide what there is to wait for.
 #include "fp4_format.h"

@@ -22,13 +22,15 @@
 // add the one before it to the output stand the exponentials of the one in the middle; all that happens rarely (a reference that is
 // outgrown, the last keys of a sequence) is behind one branch per block, which is not taken.
 //
-// What bounds it: 120 rows on 8 x 32 heads of 16384 keys take 260 us, 990 TFLOP/s of the products as defined (a large bf16 matrix
-// product of this card: 1200), and 300 when repeated without a pause: the clock falls to 1.85 GHz under the matrix unit's load, a
-// loop of nothing but these 14 instructions per block takes 160.  With all operands zero the same work takes 226.  240 rows of 4
-// heads on 16 x 8 key heads of 512 to 4096 keys take 59 us (36 GFLOP), 44 rows on 32 heads of 1024 keys 17.8, most of it the way to
-// the first key (8 us) and from the last one through the exchange (5 us).  One token of 4 heads on 32 x 8 key heads of 777 to 8191
-// keys takes 41 us for 157 MB, 3.8 TB/s; while all workgroups are in their loops the cache streams at 5.2 to 5.7.  The smallest
-// call takes 7.7 us, a chain of trips to memory: lengths, queries, tree rows, prefix.
+// What bounds it: 120 rows on 8 x 32 heads of 16384 keys take 264 us alone, 990 TFLOP/s of the products as defined (a large bf16
+// matrix product of this card: 1200), and 254 to 312 by how many calls follow each other: the clock falls to 1.85 GHz under the matrix
+// unit's load (five calls 254 to 258 us each, forty 302 to 311, two hundred 270); a loop of nothing but these 14 instructions per block
+// takes 160.  With all operands zero the same work takes 226.  240 rows of 4 heads on 16 x 8 key heads of 512 to 4096 keys take 59 to
+// 61 us (36 GFLOP), 44 rows on 32 heads of 1024 keys 17.9 to 18.6, most of it the way to the first key (8 us) and from the last one
+// through the exchange (5 us); there, outside the loops, is also what the compiler keeps in memory (160 bytes a lane with 128 rows,
+// 80 with 64).  One token of 4 heads on 32 x 8 key heads of 777 to 8191 keys takes 41 to 45 us for 157 MB, 3.5 to 3.8 TB/s; while all
+// workgroups are in their loops the cache streams at 5.2 to 5.7.  The smallest call takes 7.7 to 8.5 us, a chain of trips to memory:
+// lengths, queries, tree rows, prefix.  (Ranges: machines.  The pairs of figures at the rules below are of one machine and day.)
 #include <math.h>
 
 #include <atomic>
@@ -350,15 +352,15 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     }
     // One workgroup per compute unit goes through its tiles 1.4 to 1.7 times as fast as one of two, and half as many pieces are half
     // as much to exchange: two only where each has more than so many tiles (or where pieces would cross pairs otherwise).  Measured,
-    // one and two, in us: 60 nodes x 4 heads on 16 x 8 key heads of 512 keys 26.5 and 34.8, of 2048 56.4 and 57.0, of 4096 94.8 and
-    // 87; 44 nodes on 8 x 32 key heads of 1024 keys 24.8 and 30.9, of 4096 60 and 57; one token x 4 heads on 32 x 8 key heads of
-    // 1024 keys 20.2 and 24.0, of 4096 47.7 and 42.5.
+    // one and two, in us: 60 nodes x 4 heads on 16 x 8 key heads of 512 keys 26.0 and 34.0, of 2048 54.0 and 54.8, of 4096 89.5 and
+    // 82.6; 44 nodes on 8 x 32 key heads of 1024 keys 25.7 and 28.3, of 4096 57.1 and 51.6; one token x 4 heads on 32 x 8 key heads of
+    // 1024 keys 20.2 and 23.6, of 4096 45.9 and 39.8.
     constexpr int WORTH = QBP == 1 ? 8 : 24;
     // Tiles of a piece: no fewer than make its share of the exchange worth while.  Of t tiles in pieces of s, s are one after the
     // other, and so are the t / s parts that the last one folds: the sum is least at a multiple of sqrt(t).  (120 nodes on 4 key
-    // heads of 16384 keys, 257 tiles: pieces of 9 take 77 us, of 16 62.2, of 32 61.4; of 4096 keys: of 8 39.0, of 16 38.4, of 32
-    // 43.5.  44 nodes on the same: of 8 28.4 and 22.2, of 16 29.8 and 23.4.  One token on 8 key heads of 4096 keys, 33 tiles: of 2
-    // 16.9, of 4 17.8, of 8 19.5.)
+    // heads of 16384 keys, 257 tiles: pieces of 9 take 78 us, of 16 62.5, of 32 60.5; of 4096 keys: of 8 39.6, of 16 38.5, of 32
+    // 43.2.  44 nodes on the same: of 8 28.4 and 22.0, of 16 30.1 and 22.7.  One token x 4 heads on 8 key heads of 4096 keys, 33 tiles:
+    // of 2 17.8, of 4 18.2, of 8 19.7.)
     const int least = max(max(C::MIN_TILES, (int)(C::FOLD * __builtin_amdgcn_sqrtf((float)most))), (most + MAX_SPLITS - 1) / MAX_SPLITS);
     int per = 0, aligned = 0;                                          // aligned > 0: pieces of at most that many tiles, none crosses a pair
     for (int all = total * p.units >= 2 * p.single * WORTH; all < 2 && !aligned; ++all) {
@@ -370,7 +372,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         } else if (p.B <= 64) {
             // The smallest size whose splits fit the grid, unless it is so much more than an equal piece that crossing costs less.
             // (A piece of the next pair starts from nothing: 15 to 20 us.  The batch of 16 sequences of 512 to 4096 keys under 60
-            // nodes takes 62 us in pieces of 24 tiles and 70 in equal ones of 19; 32 of 777 to 8191 keys with a token each 48.5, 53.)
+            // nodes takes 61 us in pieces of 24 tiles and 71 in equal ones of 19; 32 of 777 to 8191 keys with a token each 44.5, 60.  How
+            // much more is looked at: nothing 73 and 61 us, half of it 62 and 44, this 61 and 44.5, twice 62 and 45.)
             const int t = len_l >= 0 ? tiles_of(len_l) : 0;
             auto fits = [&](int size) { return wave_last(wave_scan(small_div(t + size - 1, size))) * p.units <= resident; };
             int lo = per, hi = per + per / 8 + (QBP == 1 ? 12 : 8) * (1 + all);
@@ -398,9 +401,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     };
     // Or whole pairs to every workgroup, the longest first, back and forth over the workgroups, where the fullest of them (of 64 looked
     // at) has less to do than one with an equal piece, which begins and ends within pairs.  Equal pieces and whole pairs, us: 44 nodes
-    // on 64 x 32 heads of 100 to 2000 keys 266 and 134, on 20 x 20 of 10 to 3000 107 and 43; 60 nodes x 4 heads on 64 x 8 key heads of
-    // 100 to 2000 170 and 98, on 32 x 8 of 100 to 4000 158 and 98; one token on 64 x 32 heads of 100 to 2000 keys 176 and 95, of 4
-    // heads on 128 x 8 key heads of 100 to 4000 124 and 79.
+    // on 64 x 32 heads of 100 to 2000 keys 269 and 132; 60 nodes x 4 heads on 64 x 8 key heads of 100 to 2000 169 and 100, on 32 x 8 of
+    // 100 to 4000 155 and 98; one token on 64 x 32 heads of 100 to 2000 keys 184 and 96, of 4 heads on 128 x 8 key heads of 100 to 4000
+    // 124 and 76.  With more than 32 pairs to a workgroup always: one token on 256 x 80 heads of 64, of 100 to 900 keys, 630 and 417, of
+    // 500 keys each 382 and 395.
     constexpr int BEGIN = 5, CROSS = QBP == 4 ? 24 : 16;               // tiles that a new pair costs, and one that is begun or ended within
     const int pairs = p.B * p.units;
     int rounds = 0;                                                    // > 0: of whole pairs
@@ -432,7 +436,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         if (aligned && p.B <= 64) {
             // Pieces of different sizes, two to a compute unit: the sequences by the size of their pieces, the first half of the
             // workgroups takes them from the largest on, the second half from the smallest on (workgroups come to the compute
-            // units in turn, so the longest piece shares with the shortest: 41.9 us instead of 45.3 for 32 sequences of 777 to 8191
+            // units in turn, so the longest piece shares with the shortest: 44.5 us instead of 49.2 for 32 sequences of 777 to 8191
             // keys with a token each).
             const int pieces = wave_last(wave_scan(each * p.units));
             if (__builtin_expect(pieces > p.single, 0)) {
@@ -741,8 +745,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
             }
         }
         // (The first tiles are requested only now: the compiler's waits for queries and tree rows would be waits for them too, and at
-        // the start all workgroups' requests queue for memory together.  One token for 32 sequences of 777 to 8191 keys 42.4 us
-        // instead of 45, 60 nodes on 16 x 8 key heads of 512 to 4096 keys 59.6 instead of 62.)
+        // the start all workgroups' requests queue for memory together.  One token for 32 sequences of 777 to 8191 keys 44.4 us
+        // instead of 45.4, 60 nodes on 16 x 8 key heads of 512 to 4096 keys 61 instead of 62.6; for calls of one to eight tiles it makes
+        // no difference: 8.5 and 8.6, 12.5 and 12.4, 14.9 and 14.8, 16.6 and 16.6, 18.5 and 18.6.)
 #pragma unroll
         for (int x = 0; x < C::AHEAD; ++x)
             if (x < n_pre) issue(x, x * C::STAGE);
@@ -1083,8 +1088,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
                     if ((int)*s_prev + 1 == n_pieces) {
                         if (tid == 0) __hip_atomic_store(p.ctr + (int64_t)first_piece * CTR_STRIDE, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
                         // NF pieces at a time, everything of them requested at once; beyond the last one loads give zero.  As many as the
-                        // registers hold (64 rows: with 4 at a time 44 nodes on 32 heads of 1024 keys, five pieces, take 18.9 us, with 5
-                        // 17.9, with 6, which do not fit beside the rest, 20.8).
+                        // registers hold (64 rows: with 4 at a time 44 nodes on 32 heads of 1024 keys, five pieces, take 19.3 us, with 5
+                        // 18.5, with 6, which do not fit beside the rest, 21.1).
                         constexpr int NF = C::PP >= 16 ? 2 : C::PP == 8 ? 5 : 8;
                         const auto off_of = [&](int i) { return (2 * i + (i == 0)) * ROWS; };
                         const auto rm = __builtin_amdgcn_make_buffer_rsrc((void *)(p.part_m + (int64_t)2 * first_piece * ROWS), 0, 2 * n_pieces * ROWS * 4, 0x00027000);
@@ -1175,9 +1180,10 @@ int compute_units()
 bool make_plan(int B, int H_kv, int grp, int d, int n_rows, int n, int max_prefix, Fp4Plan &pl)
 {
     const int64_t rows = (int64_t)grp * n_rows;
-    // As few blocks of 32 rows as hold them.  One token of 4 heads on 32 x 8 key heads of 777 to 8191 keys: one block 44 us, two 56; 44
-    // rows on 32 heads of 1024 keys: two 18.2, four 22.4, on 8 x 32 of 4096 55 and 71; 240 rows on 16 x 8 key heads of 512 to 4096
-    // keys: four 60, two (twice the chunks) 72; 120 rows on 8 x 32 heads of 16384 keys: four 252, two 310.
+    // As few blocks of 32 rows as hold them.  One token of 4 heads on 32 x 8 key heads of 777 to 8191 keys: one block 44.5 us, two 55; 44
+    // rows on 32 heads of 1024 keys: two 18.5, four 23.0, on 8 x 32 of 4096 52 and 69; 240 rows on 16 x 8 key heads of 512 to 4096
+    // keys: four 61, two (twice the chunks) 72, of 2048 keys each 54.3 and 53.7; 120 rows on 8 x 32 heads of 16384 keys: four 264,
+    // two 321.
     pl.QBP = rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
     const int64_t chunks = (rows + 32 * pl.QBP - 1) / (32 * pl.QBP), units = chunks * H_kv;
     const int T = pl.QBP == 1 ? 128 : 64;
