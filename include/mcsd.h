@@ -390,7 +390,7 @@ int mcsd_commit_path(const mcsd_mask_view_t *mask, mcsd_dtype_t dtype, int32_t B
  * k_codes, k_scales, v_codes, v_scales : DEVICE uint8.  Row j of head h of sequence b starts at code byte
  *      (seq_base[b] + h*head_stride + j*d) / 2 and scale byte (seq_base[b] + h*head_stride + j*d) / 32: offsets are in
  *      channels, as in the other caches.  head_stride and every seq_base[b] are multiples of 128 channels, code arrays are
- *      16-byte and scale arrays 4-byte aligned.
+ *      16-byte and scale arrays 4-byte aligned.  Scales are read 4 bytes at a time: with d 64 a head has an even number of rows.
  * ------------------------------------------------------------------------------------------------- */
 typedef struct mcsd_fp4_cache {
     void *k_codes;
@@ -441,7 +441,8 @@ int mcsd_store_fp4kv(mcsd_dtype_t dtype, int32_t B, int32_t H, int32_t d, int32_
 
 /* The reverse, for n_layers layers in one launch: the numbers that cache rows first_row[b] + t stand for (exact in bf16 but for
  * the ends of its range) become row t of head h of sequence b of the layer's k and v.  Rows that are skipped are not written.
- * caches : HOST array [n_layers];   k, v : HOST arrays [n_layers] of DEVICE pointers, addressed as in mcsd_store_fp4kv
+ * caches : HOST array [n_layers];   k, v : HOST arrays [n_layers] of DEVICE pointers, addressed as in mcsd_store_fp4kv; rows must
+ *          not share places, so a stride below d is MCSD_EINVAL where there is more than one of its kind (B, H, max_rows)
  * Limits and errors as mcsd_store_fp4kv; 1 <= n_layers <= MCSD_COMMIT_MAX_LAYERS (more: MCSD_EUNSUPPORTED). */
 int mcsd_load_fp4kv(mcsd_dtype_t dtype, int32_t B, int32_t H, int32_t d, int32_t n_layers, int32_t max_rows,
                     const mcsd_fp4_cache_t *caches, const int64_t *seq_base_dev, int64_t head_stride, int32_t capacity,

@@ -164,6 +164,8 @@ extern "C" int mcsd_load_fp4kv(mcsd_dtype_t dtype, int32_t B, int32_t H, int32_t
     const int rc = check_rows(dtype, B, H, d, max_rows, batch_stride, dst_head_stride, row_stride, first_row_dev, n_rows_dev, seq_base_dev,
                               head_stride, capacity, grid_x);
     if (rc != MCSD_OK) return rc;
+    // (a tensor expanded over one of its dimensions would be written by several rows at once)
+    if ((B > 1 && batch_stride < d) || (H > 1 && dst_head_stride < d) || (max_rows > 1 && row_stride < d)) return MCSD_EINVAL;
     if (n_layers > MCSD_COMMIT_MAX_LAYERS) return MCSD_EUNSUPPORTED;
     LoadParams p;
     for (int l = 0; l < MCSD_COMMIT_MAX_LAYERS; ++l) {

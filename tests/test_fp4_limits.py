@@ -20,6 +20,14 @@ def test_rows_beyond_a_launch_are_refused(d, H):
         assert _load(d=d, H=H, rows=rows) == b.MCSD_EUNSUPPORTED, rows
 
 
+@pytest.mark.parametrize("wrong", [dict(bs=0), dict(hs=0), dict(rs=0), dict(rs=120), dict(hs=64), dict(bs=8)])
+def test_rows_are_not_read_into_one_place(wrong):
+    """An expanded tensor can be stored from, not loaded into; with one of a kind its stride says nothing."""
+    assert _load(**wrong) == b.MCSD_EINVAL
+    assert _load(B=1, H=1, rows=1, bs=0, hs=0, rs=0, layers=65) == b.MCSD_EUNSUPPORTED           # (refused for the layers alone)
+    assert _store(bs=0, hs=0, rs=0, d=32) == b.MCSD_EUNSUPPORTED                                 # (for d alone)
+
+
 @pytest.mark.parametrize("Hq,Hkv", [(4, 2), (32, 8), (1, 1)])
 def test_prompts_beyond_a_launch_are_refused(Hq, Hkv):
     """Four rows per workgroup where one would be too many workgroups."""
