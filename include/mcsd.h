@@ -505,6 +505,106 @@ int mcsd_prompt_qk_norm_rope(mcsd_dtype_t dtype, int32_t B, int32_t H_q, int32_t
                              int64_t out_row_stride, void *hip_stream);
 
 /* ---------------------------------------------------------------------------------------------------
+ * A prefix cache of one latent vector per token (beyond the paper's setting): models whose keys and values of all heads are
+ * projections of one shared vector.  Its row holds d_latent channels c and d_rope channels r that carry the position.  With the
+ * heads' key projections absorbed into the queries and their value projections into what follows, a row is the key of every
+ * head (all its channels) and its value (the first d_latent):
+ *     out[b][h][i] = sum_j softmax_j(softmax_scale * <q_hi, x_j>) * x_j[0 .. d_latent-1]
+ * over all prefix rows j < prefix_lens[b] and all tree rows j whose mask bit (i, j) is set.  (The expanded form, a key and a value per
+ * head made from each row, needs fewer operations only from 171 query rows per head on, for heads of 128 + 64 and 128 channels; a
+ * tree has up to MCSD_ATTN_MAX_NODES.)  A row is d_latent + d_rope bf16 numbers; the sizes are 512 + 64 or 256 + 32.
+ *
+ * q             : DEVICE bf16 [B][H][node_stride][d_latent + d_rope], rows row_begin .. n_nodes-1 of each (b,h) are read
+ * latent_tree   : DEVICE bf16 [B][node_stride][d_latent + d_rope], the tree nodes' rows
+ * latent_prefix : DEVICE bf16; element (b,j,c) at seq_base[b] + j*(d_latent + d_rope) + c; may be NULL where max_prefix is 0
+ * out           : DEVICE bf16 [B][H][node_stride][d_latent]; rows row_begin .. n_nodes-1 are written, nothing else
+ * Limits: 16-byte aligned tensors, seq_base multiples of 8 elements; 1 <= n_nodes <= MCSD_ATTN_MAX_NODES; softmax_scale finite and > 0.
+ * workspace     : DEVICE, mcsd_tree_attention_latent_workspace(...) bytes (0: may be NULL), 256-byte aligned.  It needs no preparation,
+ *                 and the first 64 KiB + 256 bytes stay as they are, so a workspace of the other attention calls serves as well.  The
+ *                 size for a call serves calls of the same B, H and sizes with fewer nodes, rows or prefix keys.  Calls that share a
+ *                 workspace must be ordered on one stream.
+ * Scores, soft-max statistics and sums are fp32; weights are rounded to bf16 for the product with the values; partial results of split
+ * keys are exchanged in fp32 and folded in a fixed order.  One launch, a second one where keys may be split.
+ * Accepted rows join the cache through mcsd_commit_path with H = 1, d = d_latent + d_rope, head_stride 0 and the same arrays as keys
+ * and as values.
+ * Errors: MCSD_EUNSUPPORTED for other sizes, too many nodes, or more than 2^30 tiles of 64 rows and 64 keys; MCSD_EINVAL also for a mask
+ * of another device than the current one.
+ * ------------------------------------------------------------------------------------------------- */
+size_t mcsd_tree_attention_latent_workspace(int32_t B, int32_t H, int32_t d_latent, int32_t d_rope, int32_t n_nodes,
+                                            int32_t row_begin, int32_t max_prefix);
+
+int mcsd_tree_attention_latent(const mcsd_mask_view_t *mask, int32_t B, int32_t H, int32_t d_latent, int32_t d_rope,
+                               int32_t row_begin, const void *q, const void *latent_tree, int64_t node_stride,
+                               const void *latent_prefix, const int64_t *seq_base_dev, const int32_t *prefix_lens_dev,
+                               int32_t max_prefix, float softmax_scale, void *out, void *workspace, size_t workspace_bytes,
+                               void *hip_stream);
+
+/* What feeds it, from the projections' output: the norm of the latent channels (over all d_latent, with rope->k_weight, none where that
+ * is NULL), the rotation of the d_rope channels by position, rounded to bf16 once; formulas and precision as in mcsd_tree_qk_norm_rope.
+ *
+ * mcsd_tree_latent_norm_rope : rows are tree nodes row_begin .. n_nodes-1 (input row t is node row_begin + t) at position
+ *                    L_b + level(i) - 1, L_b = prefix_lens[b] clamped to 0..max_prefix.  Rows row_begin .. n_nodes-1 of latent_out
+ *                    [B][node_stride][d_latent + d_rope] are written, and the queries' rotated channels into channels d_latent .. of
+ *                    the same rows of q_out [B][H][node_stride][d_latent + d_rope]; nothing else (the other channels of q_out are the
+ *                    absorbed queries').
+ * mcsd_store_latent : a prompt's rows into the cache: cache row first_row[b] + t, t = 0 .. n_rows[b]-1 (n_rows clamped to 0..max_rows), at
+ *                    the position of the same number; rows outside 0..capacity-1 are skipped, never touched.
+ * dtype         : element type of q_in and kv_in (MCSD_F32 or MCSD_BF16); outputs are bf16.  Inputs and outputs must not overlap.
+ * q_in          : DEVICE; element (b, t, h, c), c < d_rope, at b*q_batch_stride + t*q_row_stride + h*q_head_stride + c
+ * kv_in         : DEVICE; element (b, t, c), c < d_latent + d_rope, at b*kv_batch_stride + t*kv_row_stride + c
+ * rope          : HOST struct; q_weight must be NULL, k_weight DEVICE fp32 [d_latent] or NULL, 16-byte aligned; rotary_dim a multiple of
+ *                 16 in 0..d_rope, the first so many of the d_rope channels are rotated
+ * cache, seq_base_dev : as latent_prefix above;   capacity : rows every sequence of the cache can hold
+ * Limits: 16-byte aligned tensors, strides >= 0 and multiples of 8 elements, seq_base multiples of 8; max_rows < 2^24.  One launch, no
+ * workspace; max_rows == 0 does nothing. */
+int mcsd_tree_latent_norm_rope(const mcsd_mask_view_t *mask, mcsd_dtype_t dtype, int32_t B, int32_t H, int32_t d_latent,
+                               int32_t d_rope, int32_t row_begin, const void *q_in, const void *kv_in, int64_t q_batch_stride,
+                               int64_t q_row_stride, int64_t q_head_stride, int64_t kv_batch_stride, int64_t kv_row_stride,
+                               const mcsd_rope_t *rope, const int32_t *prefix_lens_dev, int32_t max_prefix, void *q_out,
+                               void *latent_out, int64_t node_stride, void *hip_stream);
+
+int mcsd_store_latent(mcsd_dtype_t dtype, int32_t B, int32_t d_latent, int32_t d_rope, int32_t max_rows, const void *kv_in,
+                      int64_t kv_batch_stride, int64_t kv_row_stride, const mcsd_rope_t *rope, const int32_t *first_row_dev,
+                      const int32_t *n_rows_dev, void *cache, const int64_t *seq_base_dev, int32_t capacity, void *hip_stream);
+
+/* ---------------------------------------------------------------------------------------------------
+ * From logits to the rows that the verification takes (p_target, q_draft), and tokens drawn from them (a tree's level, a target's first
+ * level, plain decoding).
+ *
+ * The tokens of a row are ordered by logit, largest first, equal ones by index, lowest first.  With x the logits, T the temperature and
+ * w_i = exp((x_i - max x) / T), a token is kept if it is
+ *     top-k : among the first top_k                                             (off where top_k <= 0)
+ *     top-p : the first, or w of all tokens before it sums to less than top_p times the sum over those that top-k keeps  (off: >= 1)
+ *     min-p : w_i >= min_p                                                      (off where min_p <= 0; above 1 it counts as 1)
+ * and its logit is not minus infinity.  p_i = w_i / (sum of the kept w) for kept tokens, 0 for others.  T = 0 keeps the first token alone.
+ * Borders and draws are decided by the w to within 2^-46 of the largest; probabilities are fp32.
+ * Draw d of a row is the first kept token, in the order of indices, at which the running sum of w exceeds u[d] times all of it; with
+ * MCSD_WITHOUT_REPLACEMENT the tokens drawn before it are left out of both.  A draw that finds nothing left is -1.
+ * A row of minus infinities alone has zero probabilities and tokens -1; one with a NaN or plus infinity, or with T or top_p or min_p
+ * NaN or T < 0, has NaN probabilities and tokens -1.
+ *
+ * logits  : DEVICE, dtype MCSD_F32 or MCSD_BF16; element (b, r, v) at b*batch_stride + r*row_stride + v, r < W, v < V; rows may begin at
+ *           any element
+ * sampler : HOST struct of DEVICE arrays, one value per sequence: temperature, top_p, min_p fp32 [B], top_k int32 [B]; NULL: 1, off, off, off
+ * probs   : DEVICE fp32, row r of sequence b at b*probs_batch_stride + r*V, as mcsd_verify_tree takes them; NULL: not written
+ * u       : DEVICE fp32 [B][W*n_draw] in [0,1)  (kept within it);   0 <= n_draw <= MCSD_MAX_BRANCH
+ * tokens  : DEVICE int32; draw d of row r of sequence b at b*tokens_batch_stride + r*n_draw + d: with the rows of a level's contexts in
+ *           node order, and tokens pointing at the next level's first node, the children of each context
+ * Limits: V <= MCSD_MAX_VOCAB, W < 2^22.  Rows that are written must not share places (MCSD_EINVAL).  One launch, no workspace.
+ * ------------------------------------------------------------------------------------------------- */
+typedef struct mcsd_sampler {
+    const float *temperature;
+    const int32_t *top_k;
+    const float *top_p;
+    const float *min_p;
+} mcsd_sampler_t;
+
+int mcsd_sample_rows(mcsd_dtype_t dtype, int32_t B, int32_t W, int32_t V, const void *logits, int64_t batch_stride,
+                     int64_t row_stride, const mcsd_sampler_t *sampler, float *probs, int64_t probs_batch_stride,
+                     mcsd_sampling_t sampling, int32_t n_draw, const float *u, int32_t *tokens, int64_t tokens_batch_stride,
+                     void *hip_stream);
+
+/* ---------------------------------------------------------------------------------------------------
  * Early-stop decision models (Sec. 3.3; threshold beta = 0.4 in the caption of Fig. 2)
  *
  * After a draft-generation turn a small MLP predicts, for each of the W candidate sequences of each of B trees,

@@ -28,7 +28,9 @@ EXPORTS = ["mcsd_strerror", "mcsd_build_mask", "mcsd_slice_mask", "mcsd_free_mas
            "mcsd_early_stop_hidden", "mcsd_profile_next", "mcsd_stream_read", "mcsd_issue_probe", "mcsd_placement_probe", "mcsd_workspace_init",
            "mcsd_tree_attention_tuned_workspace", "mcsd_tree_attention_tuned", "mcsd_tree_attention_static",
            "mcsd_tree_attention_plan", "mcsd_tree_attention_fp4kv_workspace", "mcsd_tree_attention_fp4kv", "mcsd_store_fp4kv",
-           "mcsd_load_fp4kv", "mcsd_commit_path_fp4kv", "mcsd_tree_qk_norm_rope", "mcsd_prompt_qk_norm_rope"]
+           "mcsd_load_fp4kv", "mcsd_commit_path_fp4kv", "mcsd_tree_qk_norm_rope", "mcsd_prompt_qk_norm_rope",
+           "mcsd_tree_attention_latent_workspace", "mcsd_tree_attention_latent", "mcsd_tree_latent_norm_rope", "mcsd_store_latent",
+           "mcsd_sample_rows"]
 STATIC_SCRATCH_BYTES = 24 * 1024 * 1024
 DECISION_MAX_K, MLP_MAX_LAYERS, MLP_MAX_WIDTH, MLP_MAX_INPUTS = 16, 3, 512, 8192
 
@@ -76,6 +78,11 @@ class Rope(C.Structure):
     """mcsd_rope_t"""
     _fields_ = [("rotary_dim", C.c_int32), ("interleaved", C.c_int32), ("eps", C.c_float), ("inv_freq", C.c_void_p),
                 ("q_weight", C.c_void_p), ("k_weight", C.c_void_p)]
+
+
+class Sampler(C.Structure):
+    """mcsd_sampler_t"""
+    _fields_ = [("temperature", C.c_void_p), ("top_k", C.c_void_p), ("top_p", C.c_void_p), ("min_p", C.c_void_p)]
 
 
 class McsdError(RuntimeError):
@@ -184,6 +191,18 @@ def _load() -> C.CDLL:
     lib.mcsd_prompt_qk_norm_rope.restype = C.c_int
     lib.mcsd_prompt_qk_norm_rope.argtypes = [C.c_int, i32, i32, i32, i32, i32, vp, vp, vp, i64, i64, i64, i64, C.POINTER(Rope),
                                              vp, vp, vp, vp, vp, i64, vp]
+    lib.mcsd_tree_attention_latent_workspace.restype = sz
+    lib.mcsd_tree_attention_latent_workspace.argtypes = [i32] * 7
+    lib.mcsd_tree_attention_latent.restype = C.c_int
+    lib.mcsd_tree_attention_latent.argtypes = [C.POINTER(MaskView), i32, i32, i32, i32, i32, vp, vp, i64, vp, vp, vp, i32, C.c_float,
+                                               vp, vp, sz, vp]
+    lib.mcsd_tree_latent_norm_rope.restype = C.c_int
+    lib.mcsd_tree_latent_norm_rope.argtypes = [C.POINTER(MaskView), C.c_int, i32, i32, i32, i32, i32, vp, vp, i64, i64, i64, i64, i64,
+                                               C.POINTER(Rope), vp, i32, vp, vp, i64, vp]
+    lib.mcsd_store_latent.restype = C.c_int
+    lib.mcsd_store_latent.argtypes = [C.c_int, i32, i32, i32, i32, vp, i64, i64, C.POINTER(Rope), vp, vp, vp, vp, i32, vp]
+    lib.mcsd_sample_rows.restype = C.c_int
+    lib.mcsd_sample_rows.argtypes = [C.c_int, i32, i32, i32, vp, i64, i64, C.POINTER(Sampler), vp, i64, C.c_int, i32, vp, vp, i64, vp]
     return lib
 
 
@@ -225,7 +244,7 @@ def _load_pycall():
     def setup(get_device):
         mod.setup(tuple(C.cast(getattr(lib, n), C.c_void_p).value for n in mod.names()), torch.Tensor,
                   torch._C._cuda_getCurrentRawStream, get_device, _raise, MaskView, Mlp, Fp4Cache, Rope,
-                  C.ArgumentError)
+                  Sampler, C.ArgumentError)
 
     setup(device)
     return mod
@@ -546,6 +565,57 @@ def prompt_qk_norm_rope(dtype: int, B: int, H_q: int, H_kv: int, d: int, max_row
     _weights_of(rope, d, "mcsd_prompt_qk_norm_rope")
     _pycall.prompt_qk_norm_rope(dtype, B, H_q, H_kv, d, max_rows, q_in, k_in, v_in, q_batch_stride, q_row_stride, kv_batch_stride,
                                 kv_row_stride, rope, first_pos_dev, n_rows_dev, q_out, k_out, v_out, out_row_stride, stream)
+
+
+def tree_attention_latent_workspace(B: int, H: int, d_latent: int, d_rope: int, n_nodes: int, row_begin: int, max_prefix: int) -> int:
+    return int(lib.mcsd_tree_attention_latent_workspace(B, H, d_latent, d_rope, n_nodes, row_begin, max_prefix))
+
+
+def tree_attention_latent(view: MaskView, B: int, H: int, d_latent: int, d_rope: int, row_begin: int, q: torch.Tensor,
+                          latent_tree: torch.Tensor, node_stride: int, latent_prefix: Optional[torch.Tensor], seq_base_dev: torch.Tensor,
+                          prefix_lens_dev: torch.Tensor, max_prefix: int, softmax_scale: float, out: torch.Tensor,
+                          workspace: Optional[torch.Tensor], stream=None) -> None:
+    _pycall.tree_attention_latent(view, B, H, d_latent, d_rope, row_begin, q, latent_tree, node_stride, latent_prefix, seq_base_dev,
+                                  prefix_lens_dev, max_prefix, softmax_scale, out, workspace, stream)
+
+
+def tree_latent_norm_rope(view: MaskView, dtype: int, B: int, H: int, d_latent: int, d_rope: int, row_begin: int, q_in: torch.Tensor,
+                          kv_in: torch.Tensor, q_batch_stride: int, q_row_stride: int, q_head_stride: int, kv_batch_stride: int,
+                          kv_row_stride: int, rope: Rope, prefix_lens_dev: torch.Tensor, max_prefix: int, q_out: torch.Tensor,
+                          latent_out: torch.Tensor, node_stride: int, stream=None) -> None:
+    _weights_of(rope, d_latent, "mcsd_tree_latent_norm_rope")
+    _pycall.tree_latent_norm_rope(view, dtype, B, H, d_latent, d_rope, row_begin, q_in, kv_in, q_batch_stride, q_row_stride, q_head_stride,
+                                  kv_batch_stride, kv_row_stride, rope, prefix_lens_dev, max_prefix, q_out, latent_out, node_stride, stream)
+
+
+def store_latent(dtype: int, B: int, d_latent: int, d_rope: int, max_rows: int, kv_in: torch.Tensor, kv_batch_stride: int,
+                 kv_row_stride: int, rope: Rope, first_row_dev: torch.Tensor, n_rows_dev: torch.Tensor, cache: torch.Tensor,
+                 seq_base_dev: torch.Tensor, capacity: int, stream=None) -> None:
+    _weights_of(rope, d_latent, "mcsd_store_latent")
+    _pycall.store_latent(dtype, B, d_latent, d_rope, max_rows, kv_in, kv_batch_stride, kv_row_stride, rope, first_row_dev, n_rows_dev, cache,
+                         seq_base_dev, capacity, stream)
+
+
+def make_sampler(temperature: Optional[torch.Tensor] = None, top_k: Optional[torch.Tensor] = None, top_p: Optional[torch.Tensor] = None,
+                 min_p: Optional[torch.Tensor] = None) -> Sampler:
+    """mcsd_sampler_t: contiguous device tensors of one value per sequence, fp32 (top_k int32); None: 1, off, off, off."""
+    for t, dtype in ((temperature, torch.float32), (top_k, torch.int32), (top_p, torch.float32), (min_p, torch.float32)):
+        if t is not None and (t.dtype != dtype or not t.is_contiguous()):
+            raise McsdError(MCSD_EINVAL, "make_sampler (contiguous fp32 tensors, int32 for top_k)")
+    s = Sampler(_ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p))
+    s._keep = (temperature, top_k, top_p, min_p)  # the struct holds raw pointers
+    s._values = min((t.numel() for t in s._keep if t is not None), default=None)
+    return s
+
+
+def sample_rows(dtype: int, B: int, W: int, V: int, logits: torch.Tensor, batch_stride: int, row_stride: int, sampler: Sampler,
+                probs: Optional[torch.Tensor], probs_batch_stride: int, sampling: int, n_draw: int, u: Optional[torch.Tensor],
+                tokens: Optional[torch.Tensor], tokens_batch_stride: int, stream=None) -> None:
+    n = getattr(sampler, "_values", None)
+    if n is not None and n < B:                   # the kernel reads as many
+        raise McsdError(MCSD_EINVAL, f"mcsd_sample_rows (settings of fewer than {B} sequences)")
+    _pycall.sample_rows(dtype, B, W, V, logits, batch_stride, row_stride, sampler, probs, probs_batch_stride, sampling, n_draw, u, tokens,
+                        tokens_batch_stride, stream)
 
 
 def stream_read(src: torch.Tensor, sink: torch.Tensor, workgroups: int = 0, stream=None) -> None:

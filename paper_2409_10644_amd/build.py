@@ -27,7 +27,10 @@ SOURCES = {
     "verify_tree.hip": ["-ffp-contract=off"],
     "tree_attention_fp4.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
     "fp4_cache.hip": [],
+    "tree_attention_latent.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
     "qk_rope.hip": [],
+    "latent_rows.hip": [],
+    "sample_rows.hip": [],
     "commit_path.hip": [],
     "decision.hip": [],
     "probe.hip": [],

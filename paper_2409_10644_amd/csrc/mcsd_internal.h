@@ -29,6 +29,8 @@ struct McsdTreeDesc {
 
 // Workgroups of 256 lanes that one direction of a launch can have: its lanes are counted in 32 bits.
 constexpr int64_t MCSD_MAX_GRID_256 = 0xffffff;
+// ... and of 1024.
+constexpr int64_t MCSD_MAX_GRID_1024 = 0x3fffff;
 
 static inline int mcsd_hip_status(hipError_t e) { return e == hipSuccess ? MCSD_OK : MCSD_EHIP; }
 

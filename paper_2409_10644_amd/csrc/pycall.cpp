@@ -15,16 +15,17 @@
 namespace {
 
 enum Fn { ATTN, ATTN_ROWS, ATTN_GQA, ATTN_FP8, ATTN_STATIC, VERIFY, VERIFY_SAMPLING, COMMIT, STOP_DIST, STOP_HIDDEN, SLICE,
-          ATTN_FP4, STORE_FP4, LOAD_FP4, COMMIT_FP4, TREE_QK, PROMPT_QK, N_FN };
+          ATTN_FP4, STORE_FP4, LOAD_FP4, COMMIT_FP4, TREE_QK, PROMPT_QK, ATTN_LATENT, TREE_LATENT, STORE_LATENT, SAMPLE, N_FN };
 const char *const FN_NAME[N_FN] = {"mcsd_tree_attention", "mcsd_tree_attention_rows", "mcsd_tree_attention_gqa", "mcsd_tree_attention_fp8kv",
                                    "mcsd_tree_attention_static", "mcsd_verify_tree", "mcsd_verify_tree_sampling", "mcsd_commit_path",
                                    "mcsd_early_stop_distribution", "mcsd_early_stop_hidden", "mcsd_slice_mask", "mcsd_tree_attention_fp4kv",
-                                   "mcsd_store_fp4kv", "mcsd_load_fp4kv", "mcsd_commit_path_fp4kv", "mcsd_tree_qk_norm_rope", "mcsd_prompt_qk_norm_rope"};
+                                   "mcsd_store_fp4kv", "mcsd_load_fp4kv", "mcsd_commit_path_fp4kv", "mcsd_tree_qk_norm_rope", "mcsd_prompt_qk_norm_rope",
+                                   "mcsd_tree_attention_latent", "mcsd_tree_latent_norm_rope", "mcsd_store_latent", "mcsd_sample_rows"};
 void *g_fn[N_FN];
 // torch.Tensor and its methods, torch's raw stream and device getters, and what raises on a status
 PyObject *g_tensor, *g_data_ptr, *g_numel, *g_element_size, *g_raw_stream, *g_device, *g_raise;
 // the binding's structures, and ctypes' error for an argument that is another one
-PyObject *g_mask_view, *g_mlp, *g_fp4_cache, *g_rope, *g_argument_error;
+PyObject *g_mask_view, *g_mlp, *g_fp4_cache, *g_rope, *g_sampler, *g_argument_error;
 PyObject *g_str_data_ptr, *g_str_cuda_stream, *g_str_numel, *g_str_element_size;
 
 int64_t call_int(PyObject *method, PyObject *name, PyObject *self)
@@ -423,6 +424,77 @@ PyObject *py_qk(PyObject *, PyObject *const *args, Py_ssize_t nargs)
     }
 }
 
+PyObject *py_attention_latent(PyObject *, PyObject *const *args, Py_ssize_t nargs)
+{
+    Args a(args, nargs, 17);
+    auto view = (const mcsd_mask_view_t *)a.structure(g_mask_view);
+    const int32_t B = a.i32(), H = a.i32(), dl = a.i32(), dr = a.i32(), row = a.i32();
+    void *q = a.tensor(), *tree = a.tensor();
+    const int64_t node_stride = a.integer();
+    void *prefix = a.tensor();
+    auto base = (const int64_t *)a.tensor();
+    auto lens = (const int32_t *)a.tensor();
+    const int32_t max_prefix = a.i32();
+    const float scale = a.f32();
+    void *out = a.tensor();
+    size_t ws_bytes;
+    void *ws = a.workspace(ws_bytes);
+    void *st = a.stream();
+    MCSD_UNLOCKED(mcsd_tree_attention_latent, ATTN_LATENT, view, B, H, dl, dr, row, q, tree, node_stride, prefix, base, lens, max_prefix, scale, out, ws, ws_bytes, st);
+}
+
+PyObject *py_tree_latent(PyObject *, PyObject *const *args, Py_ssize_t nargs)
+{
+    Args a(args, nargs, 21);
+    auto view = (const mcsd_mask_view_t *)a.structure(g_mask_view);
+    const auto dtype = (mcsd_dtype_t)a.i32();
+    const int32_t B = a.i32(), H = a.i32(), dl = a.i32(), dr = a.i32(), row = a.i32();
+    void *q = a.tensor(), *kv = a.tensor();
+    const int64_t qb = a.integer(), qr = a.integer(), qh = a.integer(), kvb = a.integer(), kvr = a.integer();
+    auto rope = (const mcsd_rope_t *)a.structure(g_rope);
+    auto lens = (const int32_t *)a.tensor();
+    const int32_t max_prefix = a.i32();
+    void *qo = a.tensor(), *out = a.tensor();
+    const int64_t node_stride = a.integer();
+    void *st = a.stream();
+    MCSD_UNLOCKED(mcsd_tree_latent_norm_rope, TREE_LATENT, view, dtype, B, H, dl, dr, row, q, kv, qb, qr, qh, kvb, kvr, rope, lens, max_prefix, qo, out, node_stride, st);
+}
+
+PyObject *py_store_latent(PyObject *, PyObject *const *args, Py_ssize_t nargs)
+{
+    Args a(args, nargs, 15);
+    const auto dtype = (mcsd_dtype_t)a.i32();
+    const int32_t B = a.i32(), dl = a.i32(), dr = a.i32(), rows = a.i32();
+    void *kv = a.tensor();
+    const int64_t bs = a.integer(), rs = a.integer();
+    auto rope = (const mcsd_rope_t *)a.structure(g_rope);
+    auto first = (const int32_t *)a.tensor(), n = (const int32_t *)a.tensor();
+    void *cache = a.tensor();
+    auto base = (const int64_t *)a.tensor();
+    const int32_t capacity = a.i32();
+    void *st = a.stream();
+    MCSD_UNLOCKED(mcsd_store_latent, STORE_LATENT, dtype, B, dl, dr, rows, kv, bs, rs, rope, first, n, cache, base, capacity, st);
+}
+
+PyObject *py_sample(PyObject *, PyObject *const *args, Py_ssize_t nargs)
+{
+    Args a(args, nargs, 16);
+    const auto dtype = (mcsd_dtype_t)a.i32();
+    const int32_t B = a.i32(), W = a.i32(), V = a.i32();
+    void *x = a.tensor();
+    const int64_t bs = a.integer(), rs = a.integer();
+    auto sampler = (const mcsd_sampler_t *)a.structure(g_sampler);
+    auto probs = (float *)a.tensor();
+    const int64_t pbs = a.integer();
+    const auto sampling = (mcsd_sampling_t)a.i32();
+    const int32_t n_draw = a.i32();
+    auto u = (const float *)a.tensor();
+    auto tokens = (int32_t *)a.tensor();
+    const int64_t tbs = a.integer();
+    void *st = a.stream();
+    MCSD_UNLOCKED(mcsd_sample_rows, SAMPLE, dtype, B, W, V, x, bs, rs, sampler, probs, pbs, sampling, n_draw, u, tokens, tbs, st);
+}
+
 // slice_mask(handle, gamma, view): fills the view
 PyObject *py_slice(PyObject *, PyObject *const *args, Py_ssize_t nargs)
 {
@@ -435,18 +507,18 @@ PyObject *py_slice(PyObject *, PyObject *const *args, Py_ssize_t nargs)
 }
 
 // setup(addresses of the entry points in the order of Fn, torch.Tensor, raw_stream, device, raise, MaskView, Mlp, Fp4Cache, Rope,
-// ctypes.ArgumentError)
+// Sampler, ctypes.ArgumentError)
 PyObject *py_setup(PyObject *, PyObject *args)
 {
     PyObject *addr;
-    if (!PyArg_ParseTuple(args, "O!OOOOO!O!O!O!O", &PyTuple_Type, &addr, &g_tensor, &g_raw_stream, &g_device, &g_raise, &PyType_Type, &g_mask_view,
-                          &PyType_Type, &g_mlp, &PyType_Type, &g_fp4_cache, &PyType_Type, &g_rope, &g_argument_error)) return nullptr;
+    if (!PyArg_ParseTuple(args, "O!OOOOO!O!O!O!O!O", &PyTuple_Type, &addr, &g_tensor, &g_raw_stream, &g_device, &g_raise, &PyType_Type, &g_mask_view,
+                          &PyType_Type, &g_mlp, &PyType_Type, &g_fp4_cache, &PyType_Type, &g_rope, &PyType_Type, &g_sampler, &g_argument_error)) return nullptr;
     if (PyTuple_GET_SIZE(addr) != N_FN) {
         PyErr_SetString(PyExc_ValueError, "one address per entry point");
         return nullptr;
     }
     for (int i = 0; i < N_FN; ++i) g_fn[i] = (void *)(uintptr_t)PyLong_AsUnsignedLongLongMask(PyTuple_GET_ITEM(addr, i));
-    for (PyObject *o : {g_tensor, g_raw_stream, g_device, g_raise, g_mask_view, g_mlp, g_fp4_cache, g_rope, g_argument_error}) Py_INCREF(o);       // held for the life of the process
+    for (PyObject *o : {g_tensor, g_raw_stream, g_device, g_raise, g_mask_view, g_mlp, g_fp4_cache, g_rope, g_sampler, g_argument_error}) Py_INCREF(o);       // held for the life of the process
     g_data_ptr = PyObject_GetAttr(g_tensor, g_str_data_ptr);
     g_numel = PyObject_GetAttr(g_tensor, g_str_numel);
     g_element_size = PyObject_GetAttr(g_tensor, g_str_element_size);
@@ -482,6 +554,10 @@ PyMethodDef METHODS[] = {
     FAST("commit_path_fp4kv", py_commit_fp4),
     FAST("tree_qk_norm_rope", (py_qk<TREE_QK>)),
     FAST("prompt_qk_norm_rope", (py_qk<PROMPT_QK>)),
+    FAST("tree_attention_latent", py_attention_latent),
+    FAST("tree_latent_norm_rope", py_tree_latent),
+    FAST("store_latent", py_store_latent),
+    FAST("sample_rows", py_sample),
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef MODULE = {PyModuleDef_HEAD_INIT, "_pycall", nullptr, -1, METHODS, nullptr, nullptr, nullptr, nullptr};
