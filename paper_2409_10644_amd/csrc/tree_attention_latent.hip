@@ -1,15 +1,18 @@
 // Tree attention over a prefix cache of one latent vector per token, shared by all heads (formulas in mcsd.h).
 //
-// All H * rows query rows of a sequence look at the same keys, so they are cut into chunks of 64 whichever heads they belong to,
-// and a workgroup of 4 wavefronts serves one chunk.  A tile is 64 keys; a row of it is key (all d_latent + d_rope channels) and
-// value (the first d_latent) at once, so it comes from memory and into LDS once.
-//   S^T = X Q^T   each wavefront has 16 of the tile's keys and all 64 query rows, whose operands stay in its registers
-//   P             exp2(S - reference), bf16, through LDS: every wavefront needs all of it
-//   O^T += X^T P^T  each wavefront has a quarter of the value channels, all 64 rows and all keys
-// so of a tile every number is read from LDS twice, once as key and once as value, whatever the number of rows.
+// All H * rows query rows of a sequence look at the same keys, so they are cut into chunks of 64 whichever heads they belong to, and a
+// workgroup serves one chunk.  A tile is 32 keys; a row of it is key (all d_latent + d_rope channels) and value (the first d_latent) at
+// once, so it comes from memory and into LDS once, into a ring of four tiles.
+//   S^T = X Q^T   four wavefronts, each with 16 of the tile's keys and 32 query rows, whose operands stay in its registers; then
+//   P             2^(S - reference) in bf16, through LDS
+//   O^T += X^T P^T  four others, one tile behind, each with a quarter of the value channels, all 64 rows and all keys
+// A SIMD has one wavefront of each kind: the soft-max of the one runs in the shadow of the other's products, and they meet once a tile.
+// (The same work by four wavefronts that take turns at both, alone on their SIMDs: every instruction between the products then
+// stands alone, 4500 cycles per 64 keys, of which the products are 2176.)
 #include <math.h>
 
 #include <atomic>
+#include <type_traits>
 
 #include "fp4_format.h"
 
@@ -46,9 +49,10 @@ struct LatentParams {
 };
 
 constexpr size_t WS_HEADER = 256, WS_CTR_BYTES = 64 * 1024;      // what other calls keep at the head of a workspace stays as it is
-constexpr float SLACK = 6.f;         // log2 of what a score may exceed the running reference by before the output is rescaled
-constexpr int ROWS = 64, KEYS = 64;  // query rows of a chunk, keys of a tile
-constexpr int MIN_TILES = 2, CROSS = 6;
+constexpr float SLACK = 16.f;        // log2 of what a score may exceed the running reference by before the output is rescaled
+constexpr int ROWS = 64, KEYS = 32;  // query rows of a chunk, keys of a tile
+constexpr int MIN_TILES = 4, CROSS = 12;
+constexpr int THREADS = 512;
 
 __device__ __align__(64) const unsigned char no_row[128] = {};
 
@@ -60,6 +64,22 @@ __device__ __forceinline__ const unsigned char *uniform(const unsigned char *a)
     return (const unsigned char *)((uint64_t)(uint32_t)uniform((int)(v >> 32)) << 32 | (uint32_t)uniform((int)v));
 }
 __device__ __forceinline__ void meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+__device__ __forceinline__ void bare() { asm volatile("s_barrier" ::: "memory"); }
+__device__ __forceinline__ float max4(const f32x4_t &v)
+{
+    float m;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(m) : "v"(v[0]), "v"(v[1]), "v"(v[2]));
+    asm("v_max_f32 %0, %1, %2" : "=v"(m) : "v"(m), "v"(v[3]));
+    return m;
+}
+
+// A value that the compiler knows nothing about: what is made of it is made here, not kept in registers from before the loops.
+__device__ __forceinline__ int anew(int v)
+{
+    asm volatile("" : "+v"(v));
+    return v;
+}
 
 // Over the four lanes that hold the same query row (16 apart).
 __device__ __forceinline__ float row_max(float v)
@@ -77,12 +97,49 @@ __device__ __forceinline__ float row_sum(float v)
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
-// A tile in LDS: panels of 64 channels, 128 bytes a row, 64 rows each (the last panel has the d_rope channels).  The 16-byte chunk c of row
-// r stands at c ^ swz(r): 16 rows read at one chunk, and rows 0-3 and 8-11 read at two neighbouring ones by the transpose loads, hit
-// 16 different places of a bank row.  The weights have the same form, a row's 64 keys as its 64 channels.
-__device__ __forceinline__ int swz(int r) { return ((r >> 1) & 1) << 2 | ((r >> 2) & 3); }
-// A last panel of 32 channels: 64 bytes a row.
-__device__ __forceinline__ int swz_half(int r) { return (r >> 2) & 3; }
+// Matrix products with the accumulator in its place (the builtin's result may stand elsewhere, and across a loop's branches it then
+// does: twice the registers).  The wait states that vector instructions need behind the results are the caller's: settle().
+__device__ __forceinline__ void mfma(f32x4_t &c, const bf16x8_t &a, const bf16x8_t &b) { asm("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+v"(c) : "v"(a), "v"(b)); }
+__device__ __forceinline__ void settle() { asm volatile("s_nop 15\n\ts_nop 3" ::: "memory"); }
+__device__ __forceinline__ int lds_at(const void *p) { return (int)(uintptr_t)(__attribute__((address_space(3))) const void *)p; }
+// load_to_lds16 where `ask` (uniform) is not 0, with the branch inside: in two ways around it the compiler would hold the output twice.
+template <bool NT>
+__device__ __forceinline__ void load_if(int ask, const void *gbase, uint32_t voff, void *lds_base)
+{
+    if constexpr (NT)
+        asm volatile("s_cmp_eq_u32 %3, 0\n\ts_cbranch_scc1 .Lnone%=\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt\n.Lnone%=:"
+                     : : "s"(lds_at(lds_base)), "v"(voff), "s"(gbase), "s"(ask) : "memory", "scc");
+    else
+        asm volatile("s_cmp_eq_u32 %3, 0\n\ts_cbranch_scc1 .Lnone%=\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n.Lnone%=:"
+                     : : "s"(lds_at(lds_base)), "v"(voff), "s"(gbase), "s"(ask) : "memory", "scc");
+}
+// Where `on` (uniform) is not 0, eight accumulators times the numbers at LDS bytes a (first four) and b, through 16 bytes of LDS of the
+// lane's own.  One block with its branch inside, so that for the compiler every accumulator stays in its registers: written as
+// ordinary multiplications behind a branch, it kept the output twice, and copied it from one place to the other every turn.
+#define MCSD_TIMES(C) "ds_write_b128 %9, " C "\n\ts_waitcnt lgkmcnt(0)\n\tds_read_b32 %10, %9\n\tds_read_b32 %11, %9 offset:4\n\t" \
+                      "ds_read_b32 %12, %9 offset:8\n\tds_read_b32 %13, %9 offset:12\n\ts_waitcnt lgkmcnt(0)\n\tv_mul_f32 %10, %10, %8\n\t" \
+                      "v_mul_f32 %11, %11, %8\n\tv_mul_f32 %12, %12, %8\n\tv_mul_f32 %13, %13, %8\n\tds_write_b32 %9, %10\n\t" \
+                      "ds_write_b32 %9, %11 offset:4\n\tds_write_b32 %9, %12 offset:8\n\tds_write_b32 %9, %13 offset:12\n\t" \
+                      "s_waitcnt lgkmcnt(0)\n\tds_read_b128 " C ", %9\n\ts_waitcnt lgkmcnt(0)\n\t"
+__device__ __forceinline__ void multiply(int on, f32x4_t &c0, f32x4_t &c1, f32x4_t &c2, f32x4_t &c3, f32x4_t &c4, f32x4_t &c5, f32x4_t &c6, f32x4_t &c7,
+                                         int a, int b, int own)
+{
+    float f, t0, t1, t2, t3;
+    asm volatile("s_cmp_eq_u32 %16, 0\n\ts_cbranch_scc1 .Lkept%=\n\t"
+                 "s_nop 15\n\ts_nop 3\n\tds_read_b32 %8, %14\n\ts_waitcnt lgkmcnt(0)\n\t" MCSD_TIMES("%0") MCSD_TIMES("%1") MCSD_TIMES("%2") MCSD_TIMES("%3")
+                 "ds_read_b32 %8, %15\n\ts_waitcnt lgkmcnt(0)\n\t" MCSD_TIMES("%4") MCSD_TIMES("%5") MCSD_TIMES("%6") MCSD_TIMES("%7") ".Lkept%=:"
+                 : "+v"(c0), "+v"(c1), "+v"(c2), "+v"(c3), "+v"(c4), "+v"(c5), "+v"(c6), "+v"(c7), "=&v"(f), "+v"(own), "=&v"(t0), "=&v"(t1), "=&v"(t2), "=&v"(t3)
+                 : "v"(a), "v"(b), "s"(on)
+                 : "memory", "scc");
+}
+
+// A tile in LDS: panels of 64 channels, 128 bytes a row (the last panel has the d_rope channels).  The 16-byte chunk c of row r stands at
+// c ^ swz(r), so that lanes served together hit different places of a bank row: 16-byte reads of 16 rows (served as lanes 0-3 with
+// 20-23, 4-7 with 16-19 and so on: four rows at one chunk with the next four at its neighbour; with bits 2 and 3 of the row in plain
+// order half of the cycles of these reads were conflicts) and transpose loads (rows 0-3 and 8-11 at two neighbouring chunks).
+__device__ __forceinline__ int swz(int r) { return ((r >> 1) & 1) << 2 | ((r >> 3 ^ r >> 2) & 1) << 1 | ((r >> 2) & 1); }
+// Rows of 64 bytes: a last panel of 32 channels, and the weights (a row's 32 keys).
+__device__ __forceinline__ int swz_half(int r) { return ((r >> 2) & 1) << 1 | ((r >> 3) & 1); }
 
 template <int DL_, int DR_>
 struct Cfg {
@@ -90,9 +147,11 @@ struct Cfg {
     static constexpr int KS = D / 32;                // matrix steps of S^T
     static constexpr int CB = DL / 64;               // blocks of 16 value channels of a wavefront
     static constexpr int PANELS = DL / 64, PANEL = KEYS * 128;
-    static constexpr int TILE = KEYS * ROWB;
-    static constexpr int P_AT = 2 * TILE, P_BYTES = ROWS * KEYS * 2;
-    static constexpr int MAX_AT = P_AT + P_BYTES, FLAG_AT = MAX_AT + 4 * ROWS * 4, LDS = FLAG_AT + 32;
+    static constexpr int TILE = KEYS * ROWB, STAGES = 4;
+    static constexpr int LOADS = PANELS + 1;         // per wavefront and tile
+    static constexpr int P_AT = STAGES * TILE, P_BYTES = ROWS * KEYS * 2;              // two of them
+    static constexpr int MAX_AT = P_AT + 2 * P_BYTES;                                  // two words per row: maxima, or sums
+    static constexpr int ALPHA_AT = MAX_AT + 2 * ROWS * 4, FLAG_AT = ALPHA_AT + ROWS * 4, LDS = FLAG_AT + 2 * 16;
     static_assert(LDS <= 160 * 1024 && (DR == 64 || DR == 32), "");
 };
 
@@ -118,8 +177,8 @@ __device__ __forceinline__ int wave_scan(int v, int lane)        // inclusive
     return v;
 }
 
-template <int DL, int DR>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) void tree_attn_latent_kernel(const LatentParams args)
+template <int DL, int DR, bool NT>
+__global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(2, 2))) void tree_attn_latent_kernel(const LatentParams args)
 {
     const LatentParams &p = args;
     using C = Cfg<DL, DR>;
@@ -208,21 +267,21 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
     }
 
     // ---- places of this lane
-    const int krow = 16 * wave + col;                                      // its key of the tile (operand rows), for all chunks of channels
+    const bool scorer = wave < 4;                                          // S^T and weights, else O^T
+    const int part = wave & 3, rh = part & 1, kg = part >> 1;              // a scorer's rows 32 rh .. and keys 16 kg ..; else the channels DL / 4 part ..
+    const int krow = 16 * kg + col;
     const int k_at = krow * 128 + ((grp ^ swz(krow)) << 4);                // panel's chunk grp; the other half of a panel: ^ 64
     const int k_half = C::PANELS * C::PANEL + krow * 64 + ((grp ^ swz_half(krow)) << 4);
-    const int jr = col >> 2;                                               // of the 16 lanes of a transpose load: row, 4 channels
-    const int v_row = 8 * grp + jr;                                        // + 4 for the second load, + 32 for the second step
-    const int v_at = v_row * 128 + ((((col & 3) >> 1) ^ swz(v_row)) << 4) + (col & 1) * 8 + wave * (DL / 4) * 128;
-    const int pw_at = C::P_AT + col * 128 + (((2 * wave + (grp >> 1)) ^ swz(col)) << 4) + (grp & 1) * 8;     // + 16 rows * 128 (weights written)
-    const int pr_at = C::P_AT + col * 128 + ((grp ^ swz(col)) << 4);       // (weights read; second step: ^ 64)
-    // Tile loads: 8 rows of a panel per instruction, a wavefront brings rows 16 wave .. + 15.
-    const int lrow = lane >> 3, lchunk = lane & 7;
-    const uint32_t load_even = (uint32_t)(lrow * C::ROWB + ((lchunk ^ swz(lrow)) << 4));
-    const uint32_t load_odd = (uint32_t)(lrow * C::ROWB + ((lchunk ^ swz(lrow + 8)) << 4));
-    const uint32_t load_half = (uint32_t)((lane >> 2) * C::ROWB + (((lane & 3) ^ swz_half(lane >> 2)) << 4));
+    const int pw_at = C::P_AT + (32 * rh + col) * 64 + (((2 * kg + (grp >> 1)) ^ swz_half(col)) << 4) + (grp & 1) * 8;       // weights written; + 16 rows * 64
+    const int pr_at = C::P_AT + col * 64 + ((grp ^ swz_half(col)) << 4);   // weights read
+    const int jr = col >> 2, v_row = 8 * grp + jr;                         // of the 16 lanes of a transpose load: row (+ 4 for the second load), 4 channels
+    const int v_at = v_row * 128 + ((((col & 3) >> 1) ^ swz(v_row)) << 4) + (col & 1) * 8 + part * (DL / 4) * (2 * KEYS);
+    // Tile loads, by those of O^T: 8 rows of a panel per instruction.
+    const int lrow = 8 * part + (lane >> 3);
+    const uint32_t load_at = (uint32_t)(lrow * C::ROWB + (((lane & 7) ^ swz(lrow)) << 4));
+    const int hrow = 16 * (part & 1) + (lane >> 2);                        // (half panels: 16 rows, two wavefronts bring the same)
+    const uint32_t load_half = (uint32_t)(hrow * C::ROWB + C::PANELS * 128 + (((lane & 3) ^ swz_half(hrow)) << 4));
 
-    // (begins, goes on): whether the piece's part of the unit has its first and its last tile
     for (bool begun = false;; begun = true) {
         b = uniform(b);
         chunk = uniform(chunk);
@@ -230,202 +289,255 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
         left = uniform(left);
         const int len = uniform(min(max(p.lens[b], 0), p.max_prefix)), tiles = tree_tiles + (int)(((unsigned)len + KEYS - 1) / KEYS);
         const int from = tile, count = min(left, tiles - tile);
-        const unsigned char *past = uniform((const unsigned char *)(p.cache + p.seq_base[b]));
-        const unsigned char *nodes = uniform((const unsigned char *)(p.tree + (int64_t)b * p.node_stride * C::D));
-
-        auto request = [&](int t, int stage) __attribute__((always_inline)) {
-            const unsigned char *src = t < tree_tiles ? nodes + (int64_t)t * C::TILE : past + (int64_t)(t - tree_tiles) * C::TILE;
-            const int here = t < tree_tiles ? p.n - t * KEYS : len - (t - tree_tiles) * KEYS;      // keys of this tile (or more)
-            unsigned char *dst = lds + stage * C::TILE;
-            if (here >= KEYS) {
-#pragma unroll
-                for (int k = 0; k < 2; ++k)
-#pragma unroll
-                    for (int x = 0; x < C::PANELS + (DR == 64); ++x)
-                        load_to_lds16<false>(src + (16 * wave + 8 * k) * C::ROWB + x * 128, k ? load_odd : load_even,
-                                             dst + x * C::PANEL + (16 * wave + 8 * k) * 128);
-                if constexpr (DR == 32)
-                    load_to_lds16<false>(src + 16 * wave * C::ROWB + C::PANELS * 128, load_half, dst + C::PANELS * C::PANEL + 16 * wave * 64);
-            } else {                                                       // rows behind the last: zeros
-#pragma unroll
-                for (int k = 0; k < 2; ++k)
-#pragma unroll
-                    for (int x = 0; x < C::PANELS + (DR == 64); ++x) {
-                        const int row = 16 * wave + 8 * k;
-                        load_to_lds16_at(row + lrow < here ? src + row * C::ROWB + x * 128 + (k ? load_odd : load_even) : no_row + (lane & 7) * 16,
-                                         dst + x * C::PANEL + row * 128);
-                    }
-                if constexpr (DR == 32)
-                    load_to_lds16_at(16 * wave + (lane >> 2) < here ? src + 16 * wave * C::ROWB + C::PANELS * 128 + load_half : no_row + (lane & 3) * 16,
-                                     dst + C::PANELS * C::PANEL + 16 * wave * 64);
-            }
-        };
-        request(from, 0);
-
-        // Query operands: rows col + 16 rg of the chunk (behind the last: that one), channels 32 ks + 8 grp .. + 7.  And which tree nodes
-        // the rows see among this lane's 4 keys: 4 bits per row and tree tile.
-        bf16x8_t q[4][C::KS];
-        unsigned seen[2] = {0, 0};
-#pragma unroll
-        for (int rg = 0; rg < 4; ++rg) {
-            const int r = min(chunk * ROWS + 16 * rg + col, p.rows - 1), h = row_div(r, p.by_nrows), i = p.row0 + r - h * (p.n - p.row0);
-            const uint16_t *src = p.q + (((int64_t)b * p.H + h) * p.node_stride + i) * C::D + 8 * grp;
-#pragma unroll
-            for (int ks = 0; ks < C::KS; ++ks) q[rg][ks] = *(const bf16x8_t *)(src + 32 * ks);
-            const uint64_t *bits = p.mask_bits + (int64_t)i * p.mask_words;
-            seen[0] |= (unsigned)((bits[0] >> (16 * wave + 4 * grp)) & 15) << (4 * rg);
-            if (tree_tiles > 1) seen[1] |= (unsigned)((bits[1] >> (16 * wave + 4 * grp)) & 15) << (4 * rg);
-        }
-        f32x4_t o[4][C::CB];
-        float ref[4], l[4];
-#pragma unroll
-        for (int rg = 0; rg < 4; ++rg) {
-            ref[rg] = -INFINITY;
-            l[rg] = 0.f;
-#pragma unroll
-            for (int cb = 0; cb < C::CB; ++cb) o[rg][cb] = (f32x4_t){0, 0, 0, 0};
-        }
-
-        for (int t = 0; t < count; ++t) {
-            const int at = from + t, stage = t & 1, st = stage * C::TILE;
-            MCSD_WAIT_VMCNT(0);
-            meet();                                                        // the tile is here, and the one before is done with
-            if (t + 1 < count) request(at + 1, stage ^ 1);
-
-            f32x4_t s[4];
-#pragma unroll
-            for (int rg = 0; rg < 4; ++rg) s[rg] = (f32x4_t){0, 0, 0, 0};
-#pragma unroll
-            for (int ks = 0; ks < C::KS; ++ks) {
-                const int a = DR == 32 && ks == C::KS - 1 ? k_half : (k_at ^ ((ks & 1) << 6)) + (ks >> 1) * C::PANEL;
-                const bf16x8_t k = *(const bf16x8_t *)(lds + st + a);
-#pragma unroll
-                for (int rg = 0; rg < 4; ++rg) s[rg] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[rg][ks], s[rg], 0, 0, 0);
-            }
-            const bool tree = at < tree_tiles;
-            const int here = tree ? KEYS : len - (at - tree_tiles) * KEYS;
-#pragma unroll
-            for (int rg = 0; rg < 4; ++rg) s[rg] *= p.c;
-            if (tree || here < KEYS) {
-                unsigned bits;
-                if (tree) {
-                    bits = at ? seen[1] : seen[0];
-                } else {
-                    const int mine = min(max(here - 16 * wave - 4 * grp, 0), 4);
-                    bits = ((1u << mine) - 1) * 0x1111u;
-                }
-#pragma unroll
-                for (int rg = 0; rg < 4; ++rg)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) s[rg][i] = (bits >> (4 * rg + i)) & 1 ? s[rg][i] : -INFINITY;
-            }
-            float mx[4];
-            bool grow = false;
-#pragma unroll
-            for (int rg = 0; rg < 4; ++rg) {
-                mx[rg] = fmaxf(fmaxf(s[rg][0], s[rg][1]), fmaxf(s[rg][2], s[rg][3]));
-                grow |= mx[rg] > ref[rg] + SLACK;
-            }
-            // weights, and whether a row of this wavefront outgrows its reference
-            float part[4];
-            auto weigh = [&]() __attribute__((always_inline)) {
-#pragma unroll
-                for (int rg = 0; rg < 4; ++rg) {
-                    const float zero = ref[rg] == -INFINITY ? 0.f : ref[rg];
-                    float e[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) e[i] = fast_exp2(s[rg][i] - zero);
-                    part[rg] = (e[0] + e[1]) + (e[2] + e[3]);
-                    const u32x2_t pk = {__builtin_bit_cast(unsigned, (bf16x2_t){(__bf16)e[0], (__bf16)e[1]}),
-                                        __builtin_bit_cast(unsigned, (bf16x2_t){(__bf16)e[2], (__bf16)e[3]})};
-                    *(u32x2_t *)(lds + pw_at + rg * 16 * 128) = pk;
-                }
-            };
-            weigh();
-            const bool wave_grows = __builtin_amdgcn_ballot_w64(grow) != 0;
-            if (lane == 0) *(int *)(lds + C::FLAG_AT + 4 * wave) = wave_grows;
-            meet();
-            const u32x4_t flags = *(const u32x4_t *)(lds + C::FLAG_AT);
-            if (__builtin_expect(uniform((int)(flags[0] | flags[1] | flags[2] | flags[3])) != 0, 0)) {
-                // all wavefronts: the maxima of all keys, new references, the weights again
-#pragma unroll
-                for (int rg = 0; rg < 4; ++rg) {
-                    const float m = row_max(mx[rg]);
-                    if (grp == 0) *(float *)(lds + C::MAX_AT + (wave * ROWS + 16 * rg + col) * 4) = m;
-                }
-                meet();
-#pragma unroll
-                for (int rg = 0; rg < 4; ++rg) {
-                    float m = -INFINITY;
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) m = fmaxf(m, *(const float *)(lds + C::MAX_AT + (k * ROWS + 16 * rg + col) * 4));
-                    const float next = m > ref[rg] + SLACK ? m : ref[rg];
-                    const float alpha = next == ref[rg] ? 1.f : fast_exp2(ref[rg] - next);
-                    ref[rg] = next;
-                    l[rg] *= alpha;
-#pragma unroll
-                    for (int cb = 0; cb < C::CB; ++cb) o[rg][cb] *= alpha;
-                }
-                weigh();
-                meet();
-            }
-#pragma unroll
-            for (int rg = 0; rg < 4; ++rg) l[rg] += part[rg];
-
-#pragma unroll
-            for (int k2 = 0; k2 < 2; ++k2) {
-                bf16x8_t pf[4];
-#pragma unroll
-                for (int rg = 0; rg < 4; ++rg) pf[rg] = *(const bf16x8_t *)(lds + (pr_at ^ (k2 << 6)) + rg * 16 * 128);
-#pragma unroll
-                for (int cb = 0; cb < C::CB; ++cb) {
-                    const int a = st + (v_at ^ ((cb & 3) << 5)) + (cb >> 2) * C::PANEL + k2 * 32 * 128;
-                    const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4_t __attribute__((address_space(3))) *)(lds + a));
-                    const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4_t __attribute__((address_space(3))) *)(lds + ((a + 512) ^ 16)));
-                    const bf16x8_t v = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-#pragma unroll
-                    for (int rg = 0; rg < 4; ++rg) o[rg][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pf[rg], o[rg][cb], 0, 0, 0);
-                }
-            }
-        }
-
-        // ---- sums of all wavefronts; the rows' output, or this part of it
-        meet();
-#pragma unroll
-        for (int rg = 0; rg < 4; ++rg) {
-            const float sum = row_sum(l[rg]);
-            if (grp == 0) *(float *)(lds + C::MAX_AT + (wave * ROWS + 16 * rg + col) * 4) = sum;
-        }
-        meet();
         const bool whole = from == 0 && count == tiles, first = from == 0, last = from + count == tiles;
         const int slot = aligned ? 2 * w : 2 * w + (begun ? 1 : 0);
+
+        if (scorer) {
+            // Query operands: rows col + 16 rg of this half of the chunk (behind the last: that one), channels 32 ks + 8 grp .. + 7.  And which
+            // tree nodes the rows see among this lane's 4 keys: 4 bits per row and tree tile.
+            bf16x8_t q[2][C::KS];
+            unsigned seen = 0;
 #pragma unroll
-        for (int rg = 0; rg < 4; ++rg) {
-            const int row = 16 * rg + col, r = chunk * ROWS + row;
-            float sum = 0.f;
+            for (int rg = 0; rg < 2; ++rg) {
+                const int r = min(chunk * ROWS + 32 * rh + 16 * rg + col, p.rows - 1), h = row_div(r, p.by_nrows), i = p.row0 + r - h * (p.n - p.row0);
+                const uint16_t *src = p.q + (((int64_t)b * p.H + h) * p.node_stride + i) * C::D + 8 * grp;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) sum += *(const float *)(lds + C::MAX_AT + (k * ROWS + row) * 4);
-            if (r < p.rows) {
-                if (whole) {
-                    const int h = row_div(r, p.by_nrows), i = p.row0 + r - h * (p.n - p.row0);
-                    uint16_t *dst = p.out + (((int64_t)b * p.H + h) * p.node_stride + i) * DL + wave * (DL / 4) + 4 * grp;
-                    const float inv = 1.f / sum;
+                for (int ks = 0; ks < C::KS; ++ks) q[rg][ks] = *(const bf16x8_t *)(src + 32 * ks);
+                const uint64_t *bits = p.mask_bits + (int64_t)i * p.mask_words;
+                const int at = 16 * kg + 4 * grp;
+                seen |= (unsigned)((bits[0] >> at) & 15) << (4 * rg) | (unsigned)((bits[0] >> (at + 32)) & 15) << (8 + 4 * rg);
+                if (tree_tiles > 2) seen |= (unsigned)((bits[1] >> at) & 15) << (16 + 4 * rg) | (unsigned)((bits[1] >> (at + 32)) & 15) << (24 + 4 * rg);
+            }
+            float ref[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, start[2] = {0.f, 0.f};      // (start: minus the reference, 0 while no key has been seen)
+            f32x4_t s[2];
+            // Of tile t, whose scores s holds: its maxima over all keys, new references, its weights again; what O^T has of the tiles before is
+            // multiplied by alpha.
+            auto weigh = [&](int t, float (&sum)[2]) __attribute__((always_inline)) {
+                unsigned char *pw = lds + pw_at + (t & 1) * C::P_BYTES;
 #pragma unroll
-                    for (int cb = 0; cb < C::CB; ++cb) {
-                        const f32x4_t x = o[rg][cb] * inv;
-                        const u32x2_t pk = {__builtin_bit_cast(unsigned, (bf16x2_t){(__bf16)x[0], (__bf16)x[1]}),
-                                            __builtin_bit_cast(unsigned, (bf16x2_t){(__bf16)x[2], (__bf16)x[3]})};
-                        *(u32x2_t *)(dst + 16 * cb) = pk;
+                for (int rg = 0; rg < 2; ++rg) {
+                    float e[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) e[i] = fast_exp2(fmaf(s[rg][i], p.c, start[rg]));
+                    sum[rg] = (e[0] + e[1]) + (e[2] + e[3]);
+                    const u32x2_t pk = {__builtin_bit_cast(unsigned, (bf16x2_t){(__bf16)e[0], (__bf16)e[1]}),
+                                        __builtin_bit_cast(unsigned, (bf16x2_t){(__bf16)e[2], (__bf16)e[3]})};
+                    *(u32x2_t *)(pw + rg * 16 * 64) = pk;
+                }
+            };
+            float sum[2] = {0.f, 0.f};                                     // of the last tile's weights
+            auto outgrown = [&](int t) __attribute__((always_inline)) {
+#pragma unroll
+                for (int rg = 0; rg < 2; ++rg) {
+                    const float m = row_max(max4(s[rg]) * p.c);
+                    if (grp == 0) *(float *)(lds + C::MAX_AT + (kg * ROWS + 32 * rh + 16 * rg + col) * 4) = m;
+                }
+                meet();
+#pragma unroll
+                for (int rg = 0; rg < 2; ++rg) {
+                    const int row = 32 * rh + 16 * rg + col;
+                    const float m = fmaxf(*(const float *)(lds + C::MAX_AT + row * 4), *(const float *)(lds + C::MAX_AT + (ROWS + row) * 4));
+                    const float now = m > ref[rg] + SLACK ? m : ref[rg];
+                    const float alpha = now == ref[rg] ? 1.f : fast_exp2(ref[rg] - now);
+                    ref[rg] = now;
+                    start[rg] = now == -INFINITY ? 0.f : -now;
+                    l[rg] *= alpha;
+                    if (kg == 0 && grp == 0) *(float *)(lds + C::ALPHA_AT + row * 4) = alpha;
+                }
+                weigh(t, sum);
+                meet();
+                meet();                                                    // (O^T uses the other place for weights until then)
+            };
+            auto flagged = [&](int t) __attribute__((always_inline)) { return *(const u32x4_t *)(lds + C::FLAG_AT + (t & 1) * 16); };
+            meet();                                                        // the first tile is here
+            for (int t = 0; t < count; ++t) {
+                const int at = from + t, st = (t & 3) * C::TILE, k0 = anew(k_at) + st;
+                auto key_of = [&](int ks) __attribute__((always_inline)) {
+                    return *(const bf16x8_t *)(lds + (DR == 32 && ks == C::KS - 1 ? k_half + st : (k0 ^ ((ks & 1) << 6)) + (ks >> 1) * C::PANEL));
+                };
+                const u32x4_t flags = flagged(t - 1);                      // (looked at behind the products)
+                f32x4_t n[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+                bf16x8_t kf[6];                                            // read six steps ahead
+#pragma unroll
+                for (int ks = 0; ks < 6; ++ks) kf[ks] = key_of(ks);
+                __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+                for (int ks = 0; ks < C::KS; ++ks) {
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int rg = 0; rg < 2; ++rg) mfma(n[rg], kf[ks % 6], q[rg][ks]);
+                    if (ks + 6 < C::KS) kf[ks % 6] = key_of(ks + 6);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                if (t > 0 && __builtin_expect(uniform((int)(flags[0] | flags[1] | flags[2] | flags[3])) != 0, 0)) outgrown(t - 1);
+                settle();
+#pragma unroll
+                for (int rg = 0; rg < 2; ++rg) {
+                    asm volatile("" : "+v"(n[rg]));
+                    s[rg] = n[rg];
+                    l[rg] += sum[rg];
+                }
+                const bool tree = at < tree_tiles;
+                const int here = tree ? KEYS : len - (at - tree_tiles) * KEYS;
+                if (tree || here < KEYS) {
+                    unsigned bits;
+                    if (tree) {
+                        bits = seen >> (8 * at);
+                    } else {
+                        const int mine = min(max(here - 16 * kg - 4 * grp, 0), 4);
+                        bits = ((1u << mine) - 1) * 0x11u;
                     }
-                } else {
-                    const int64_t at = (int64_t)slot * p.slot_rows + row;
-                    if (wave == 0 && grp == 0) {
-                        p.part_m[at] = ref[rg];
-                        p.part_l[at] = sum;
-                    }
-                    float *dst = p.part_o + at * DL + wave * (DL / 4) + 4 * grp;
 #pragma unroll
-                    for (int cb = 0; cb < C::CB; ++cb) *(f32x4_t *)(dst + 16 * cb) = o[rg][cb];
+                    for (int rg = 0; rg < 2; ++rg)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) s[rg][i] = (bits >> (4 * rg + i)) & 1 ? s[rg][i] : -INFINITY;
+                }
+                weigh(t, sum);
+                bool grow = false;
+#pragma unroll
+                for (int rg = 0; rg < 2; ++rg) grow |= max4(s[rg]) * p.c > ref[rg] + SLACK;
+                const bool wave_grows = __builtin_amdgcn_ballot_w64(grow) != 0;
+                if (lane == 0) *(int *)(lds + C::FLAG_AT + (t & 1) * 16 + 4 * wave) = wave_grows;
+                __builtin_amdgcn_s_setprio(0);
+                meet();
+            }
+            {
+                const u32x4_t flags = flagged(count - 1);
+                if (__builtin_expect(uniform((int)(flags[0] | flags[1] | flags[2] | flags[3])) != 0, 0)) outgrown(count - 1);
+                l[0] += sum[0];
+                l[1] += sum[1];
+            }
+            // sums and references of the rows, while O^T takes the last tile
+#pragma unroll
+            for (int rg = 0; rg < 2; ++rg) {
+                const float sum = row_sum(l[rg]);
+                const int row = 32 * rh + 16 * rg + col;
+                if (grp == 0) *(float *)(lds + C::MAX_AT + (kg * ROWS + row) * 4) = sum;
+                if (kg == 0 && grp == 0) *(float *)(lds + C::ALPHA_AT + row * 4) = ref[rg];
+            }
+            meet();
+        } else {
+            const unsigned char *past = uniform((const unsigned char *)(p.cache + p.seq_base[b]));
+            const unsigned char *nodes = uniform((const unsigned char *)(p.tree + (int64_t)b * p.node_stride * C::D));
+            auto request = [&](int t) __attribute__((always_inline)) {     // tile t of this part, LOADS loads
+                const int at = from + t, here = at < tree_tiles ? p.n - at * KEYS : len - (at - tree_tiles) * KEYS;      // keys of the tile (or more)
+                const unsigned char *src = at < tree_tiles ? nodes + (int64_t)at * C::TILE : past + (int64_t)(at - tree_tiles) * C::TILE;
+                unsigned char *dst = lds + (t & 3) * C::TILE + 8 * part * 128;
+                const int row = anew(lrow);
+                if (here >= KEYS) {
+#pragma unroll
+                    for (int x = 0; x < C::PANELS + (DR == 64); ++x) load_to_lds16<NT>(src + x * 128, load_at, dst + x * C::PANEL);
+                    if constexpr (DR == 32) load_to_lds16<NT>(src, load_half, lds + (t & 3) * C::TILE + C::PANELS * C::PANEL + 16 * (part & 1) * 64);
+                } else {                                                   // rows behind the last: zeros
+#pragma unroll
+                    for (int x = 0; x < C::PANELS + (DR == 64); ++x)
+                        load_to_lds16_at(row < here ? src + x * 128 + load_at : no_row + (anew(lane) & 7) * 16, dst + x * C::PANEL);
+                    if constexpr (DR == 32)
+                        load_to_lds16_at(hrow < here ? src + load_half : no_row + (lane & 3) * 16, lds + (t & 3) * C::TILE + C::PANELS * C::PANEL + 16 * (part & 1) * 64);
+                }
+            };
+            f32x4_t o[4][C::CB];
+#pragma unroll
+            for (int rg = 0; rg < 4; ++rg)
+#pragma unroll
+                for (int cb = 0; cb < C::CB; ++cb) o[rg][cb] = (f32x4_t){0, 0, 0, 0};
+            request(0);
+            if (count > 1) request(1);
+            if (count > 1) MCSD_WAIT_VMCNT(C::LOADS);
+            else MCSD_WAIT_VMCNT(0);
+            meet();                                                        // the first tile is here
+            // In turn t, while the scores of tile t are made, tile t - 1 is added up, tile t + 2 requested into the place of tile t - 2, and
+            // behind it tile t + 1 is here.
+            if (count > 2) request(2);
+            if (count > 2) MCSD_WAIT_VMCNT(C::LOADS);
+            else MCSD_WAIT_VMCNT(0);
+            meet();
+            for (int t = 1;; ++t) {
+                const int vb = anew(v_at) + ((t - 1) & 3) * C::TILE, pb = anew(pr_at) + ((t - 1) & 1) * C::P_BYTES;
+                auto value_of = [&](int cb) __attribute__((always_inline)) {
+                    const int a = vb ^ ((cb & 3) << 5), at = (cb >> 2) * C::PANEL;
+                    const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4_t __attribute__((address_space(3))) *)(lds + a + at));
+                    const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4_t __attribute__((address_space(3))) *)(lds + (a ^ 48) + at + 512));
+                    return __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+                };
+                const u32x4_t flags = *(const u32x4_t *)(lds + C::FLAG_AT + ((t - 1) & 1) * 16);
+                bf16x8_t pf[4], vf[4];
+#pragma unroll
+                for (int rg = 0; rg < 4; ++rg) pf[rg] = *(const bf16x8_t *)(lds + pb + rg * 16 * 64);
+#pragma unroll
+                for (int cb = 0; cb < 4; ++cb) vf[cb] = value_of(cb);
+                const int on = uniform((int)(flags[0] | flags[1] | flags[2] | flags[3]));      // whether a reference was outgrown by that tile
+                if (__builtin_expect(on != 0, 0)) {
+                    meet();
+                    meet();
+#pragma unroll
+                    for (int rg = 0; rg < 4; ++rg) pf[rg] = *(const bf16x8_t *)(lds + pb + rg * 16 * 64);
+                }
+                const int own = lds_at(lds + C::P_AT) + (t & 1) * C::P_BYTES + part * 1024 + anew(lane) * 16;      // (weights that are done with)
+                const int alpha = lds_at(lds + C::ALPHA_AT) + anew(col) * 4;
+#pragma unroll
+                for (int i = 0; i < 4 * C::CB; i += 8) {
+                    const int r0 = i / C::CB, r1 = (i + 4) / C::CB, c0 = i % C::CB, c1 = (i + 4) % C::CB;
+                    multiply(on, o[r0][c0], o[r0][c0 + 1], o[r0][c0 + 2], o[r0][c0 + 3], o[r1][c1], o[r1][c1 + 1], o[r1][c1 + 2], o[r1][c1 + 3], alpha + r0 * 64,
+                             alpha + r1 * 64, own);
+                }
+                if (on) meet();
+                const int next = t + 2, at = from + next, here = at < tree_tiles ? p.n - at * KEYS : len - (at - tree_tiles) * KEYS;
+                const unsigned char *src = at < tree_tiles ? nodes + (int64_t)at * C::TILE : past + (int64_t)(at - tree_tiles) * C::TILE;
+                unsigned char *dst = lds + (next & 3) * C::TILE;
+                int ask = uniform(next < count && here >= KEYS ? 1 : 0);
+                asm volatile("" : "+s"(ask));
+                if (next < count && !ask) request(next);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int cb = 0; cb < C::CB; ++cb) {
+#pragma unroll
+                    for (int rg = 0; rg < 4; ++rg) mfma(o[rg][cb], vf[cb % 4], pf[rg]);
+                    if (cb + 4 < C::CB) vf[cb % 4] = value_of(cb + 4);
+                    // (a load takes as long as the products of a block)
+                    load_if<NT>(ask, src + cb * 128, load_at, dst + 8 * part * 128 + cb * C::PANEL);
+                    if (cb == C::CB - 1) {
+                        if constexpr (DR == 64) load_if<NT>(ask, src + C::PANELS * 128, load_at, dst + 8 * part * 128 + C::PANELS * C::PANEL);
+                        else load_if<NT>(ask, src, load_half, dst + C::PANELS * C::PANEL + 16 * (part & 1) * 64);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                if (next < count) MCSD_WAIT_VMCNT(C::LOADS);
+                else MCSD_WAIT_VMCNT(0);
+                meet();
+                if (t == count) break;
+            }
+            // ---- the rows' output, or this part of it
+#pragma unroll
+            for (int rg = 0; rg < 4; ++rg) {
+                settle();
+#pragma unroll
+                for (int cb = 0; cb < C::CB; ++cb) asm volatile("" : "+v"(o[rg][cb]));
+                const int row = 16 * rg + anew(col), r = chunk * ROWS + row;
+                const float sum = *(const float *)(lds + C::MAX_AT + row * 4) + *(const float *)(lds + C::MAX_AT + (ROWS + row) * 4);
+                const float ref = *(const float *)(lds + C::ALPHA_AT + row * 4);
+                if (r < p.rows) {
+                    if (whole) {
+                        const int h = row_div(r, p.by_nrows), i = p.row0 + r - h * (p.n - p.row0);
+                        uint16_t *dst = p.out + (((int64_t)b * p.H + h) * p.node_stride + i) * DL + part * (DL / 4) + 4 * grp;
+                        const float inv = 1.f / sum;
+#pragma unroll
+                        for (int cb = 0; cb < C::CB; ++cb) {
+                            const f32x4_t x = o[rg][cb] * inv;
+                            const u32x2_t pk = {__builtin_bit_cast(unsigned, (bf16x2_t){(__bf16)x[0], (__bf16)x[1]}),
+                                                __builtin_bit_cast(unsigned, (bf16x2_t){(__bf16)x[2], (__bf16)x[3]})};
+                            *(u32x2_t *)(dst + 16 * cb) = pk;
+                        }
+                    } else {
+                        const int64_t at = (int64_t)slot * p.slot_rows + row;
+                        if (part == 0 && grp == 0) {
+                            p.part_m[at] = ref;
+                            p.part_l[at] = sum;
+                        }
+                        float *dst = p.part_o + at * DL + part * (DL / 4) + 4 * grp;
+#pragma unroll
+                        for (int cb = 0; cb < C::CB; ++cb) *(f32x4_t *)(dst + 16 * cb) = o[rg][cb];
+                    }
                 }
             }
         }
@@ -452,7 +564,6 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
             }
             return;
         }
-        meet();                                                            // the sums are read before the next unit's are written
         tile = 0;
         if (++chunk == p.chunks) {
             chunk = 0;
@@ -598,8 +709,10 @@ extern "C" int mcsd_tree_attention_latent(const mcsd_mask_view_t *mask, int32_t 
         p.part_o = (float *)ws;
     }
     hipStream_t st = (hipStream_t)hip_stream;
-    auto kernel = d_latent == 512 ? tree_attn_latent_kernel<512, 64> : tree_attn_latent_kernel<256, 32>;
-    mcsd_launch(MCSD_KERNEL_ATTN_SWEEP, kernel, dim3(pl.workgroups), dim3(256), st, p);
+    // (non-temporal where a sequence's keys are read once)
+    auto kernel = d_latent == 512 ? (pl.chunks == 1 ? tree_attn_latent_kernel<512, 64, true> : tree_attn_latent_kernel<512, 64, false>)
+                                  : (pl.chunks == 1 ? tree_attn_latent_kernel<256, 32, true> : tree_attn_latent_kernel<256, 32, false>);
+    mcsd_launch(MCSD_KERNEL_ATTN_SWEEP, kernel, dim3(pl.workgroups), dim3(THREADS), st, p);
     if (hipGetLastError() != hipSuccess) return MCSD_EHIP;
     if (pl.bytes > 0) {
         auto fold = d_latent == 512 ? tree_attn_latent_fold_kernel<512> : tree_attn_latent_fold_kernel<256>;
