@@ -113,23 +113,43 @@ __device__ __forceinline__ void load_if(int ask, const void *gbase, uint32_t vof
         asm volatile("s_cmp_eq_u32 %3, 0\n\ts_cbranch_scc1 .Lnone%=\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n.Lnone%=:"
                      : : "s"(lds_at(lds_base)), "v"(voff), "s"(gbase), "s"(ask) : "memory", "scc");
 }
-// Where `on` (uniform) is not 0, eight accumulators times the numbers at LDS bytes a (first four) and b, through 16 bytes of LDS of the
-// lane's own.  One block with its branch inside, so that for the compiler every accumulator stays in its registers: written as
-// ordinary multiplications behind a branch, it kept the output twice, and copied it from one place to the other every turn.
-#define MCSD_TIMES(C) "ds_write_b128 %9, " C "\n\ts_waitcnt lgkmcnt(0)\n\tds_read_b32 %10, %9\n\tds_read_b32 %11, %9 offset:4\n\t" \
-                      "ds_read_b32 %12, %9 offset:8\n\tds_read_b32 %13, %9 offset:12\n\ts_waitcnt lgkmcnt(0)\n\tv_mul_f32 %10, %10, %8\n\t" \
-                      "v_mul_f32 %11, %11, %8\n\tv_mul_f32 %12, %12, %8\n\tv_mul_f32 %13, %13, %8\n\tds_write_b32 %9, %10\n\t" \
-                      "ds_write_b32 %9, %11 offset:4\n\tds_write_b32 %9, %12 offset:8\n\tds_write_b32 %9, %13 offset:12\n\t" \
-                      "s_waitcnt lgkmcnt(0)\n\tds_read_b128 " C ", %9\n\ts_waitcnt lgkmcnt(0)\n\t"
-__device__ __forceinline__ void multiply(int on, f32x4_t &c0, f32x4_t &c1, f32x4_t &c2, f32x4_t &c3, f32x4_t &c4, f32x4_t &c5, f32x4_t &c6, f32x4_t &c7,
-                                         int a, int b, int own)
+// Where `on` (uniform) is not 0, all accumulators of a lane times the numbers at LDS bytes a, a + 64, a + 128, a + 192 (one per group of 16
+// rows), each through 16 bytes of LDS of the lane's own.  One block with its branch inside, so that for the compiler every accumulator
+// stays in its registers: written as ordinary multiplications behind a branch, it kept the output twice, and copied it from one place
+// to the other every turn.
+// (LDS serves a wavefront in order: what it wrote it reads without a wait.)
+#define MCSD_TIMES(C) "ds_write_b128 %[own], " C "\n\tds_read_b32 %[t0], %[own]\n\tds_read_b32 %[t1], %[own] offset:4\n\t" \
+                      "ds_read_b32 %[t2], %[own] offset:8\n\tds_read_b32 %[t3], %[own] offset:12\n\ts_waitcnt lgkmcnt(0)\n\tv_mul_f32 %[t0], %[t0], %[f]\n\t" \
+                      "v_mul_f32 %[t1], %[t1], %[f]\n\tv_mul_f32 %[t2], %[t2], %[f]\n\tv_mul_f32 %[t3], %[t3], %[f]\n\tds_write_b32 %[own], %[t0]\n\t" \
+                      "ds_write_b32 %[own], %[t1] offset:4\n\tds_write_b32 %[own], %[t2] offset:8\n\tds_write_b32 %[own], %[t3] offset:12\n\t" \
+                      "ds_read_b128 " C ", %[own]\n\t"
+#define MCSD_FACTOR(AT) "ds_read_b32 %[f], %[a] offset:" AT "\n\ts_waitcnt lgkmcnt(0)\n\t"
+#define MCSD_SKIP "s_cmp_eq_u32 %[on], 0\n\ts_cbranch_scc1 .Lkept%=\n\ts_nop 15\n\ts_nop 3\n\t"
+#define MCSD_TIMES4(A, B, C, D) MCSD_TIMES(A) MCSD_TIMES(B) MCSD_TIMES(C) MCSD_TIMES(D)
+__device__ __forceinline__ void multiply(int on, f32x4_t (&o)[4][4], int a, int own)
 {
     float f, t0, t1, t2, t3;
-    asm volatile("s_cmp_eq_u32 %16, 0\n\ts_cbranch_scc1 .Lkept%=\n\t"
-                 "s_nop 15\n\ts_nop 3\n\tds_read_b32 %8, %14\n\ts_waitcnt lgkmcnt(0)\n\t" MCSD_TIMES("%0") MCSD_TIMES("%1") MCSD_TIMES("%2") MCSD_TIMES("%3")
-                 "ds_read_b32 %8, %15\n\ts_waitcnt lgkmcnt(0)\n\t" MCSD_TIMES("%4") MCSD_TIMES("%5") MCSD_TIMES("%6") MCSD_TIMES("%7") ".Lkept%=:"
-                 : "+v"(c0), "+v"(c1), "+v"(c2), "+v"(c3), "+v"(c4), "+v"(c5), "+v"(c6), "+v"(c7), "=&v"(f), "+v"(own), "=&v"(t0), "=&v"(t1), "=&v"(t2), "=&v"(t3)
-                 : "v"(a), "v"(b), "s"(on)
+    asm volatile(MCSD_SKIP MCSD_FACTOR("0") MCSD_TIMES4("%0", "%1", "%2", "%3") MCSD_FACTOR("64") MCSD_TIMES4("%4", "%5", "%6", "%7")
+                 MCSD_FACTOR("128") MCSD_TIMES4("%8", "%9", "%10", "%11") MCSD_FACTOR("192") MCSD_TIMES4("%12", "%13", "%14", "%15") "s_waitcnt lgkmcnt(0)\n.Lkept%=:"
+                 : "+v"(o[0][0]), "+v"(o[0][1]), "+v"(o[0][2]), "+v"(o[0][3]), "+v"(o[1][0]), "+v"(o[1][1]), "+v"(o[1][2]), "+v"(o[1][3]),
+                   "+v"(o[2][0]), "+v"(o[2][1]), "+v"(o[2][2]), "+v"(o[2][3]), "+v"(o[3][0]), "+v"(o[3][1]), "+v"(o[3][2]), "+v"(o[3][3]),
+                   [f] "=&v"(f), [t0] "=&v"(t0), [t1] "=&v"(t1), [t2] "=&v"(t2), [t3] "=&v"(t3)
+                 : [a] "v"(a), [own] "v"(own), [on] "s"(on)
+                 : "memory", "scc");
+}
+__device__ __forceinline__ void multiply(int on, f32x4_t (&o)[4][8], int a, int own)
+{
+    float f, t0, t1, t2, t3;
+    asm volatile(MCSD_SKIP MCSD_FACTOR("0") MCSD_TIMES4("%0", "%1", "%2", "%3") MCSD_TIMES4("%4", "%5", "%6", "%7")
+                 MCSD_FACTOR("64") MCSD_TIMES4("%8", "%9", "%10", "%11") MCSD_TIMES4("%12", "%13", "%14", "%15")
+                 MCSD_FACTOR("128") MCSD_TIMES4("%16", "%17", "%18", "%19") MCSD_TIMES4("%20", "%21", "%22", "%23")
+                 MCSD_FACTOR("192") MCSD_TIMES4("%24", "%25", "%26", "%27") MCSD_TIMES4("%28", "%29", "%30", "%31") "s_waitcnt lgkmcnt(0)\n.Lkept%=:"
+                 : "+v"(o[0][0]), "+v"(o[0][1]), "+v"(o[0][2]), "+v"(o[0][3]), "+v"(o[0][4]), "+v"(o[0][5]), "+v"(o[0][6]), "+v"(o[0][7]),
+                   "+v"(o[1][0]), "+v"(o[1][1]), "+v"(o[1][2]), "+v"(o[1][3]), "+v"(o[1][4]), "+v"(o[1][5]), "+v"(o[1][6]), "+v"(o[1][7]),
+                   "+v"(o[2][0]), "+v"(o[2][1]), "+v"(o[2][2]), "+v"(o[2][3]), "+v"(o[2][4]), "+v"(o[2][5]), "+v"(o[2][6]), "+v"(o[2][7]),
+                   "+v"(o[3][0]), "+v"(o[3][1]), "+v"(o[3][2]), "+v"(o[3][3]), "+v"(o[3][4]), "+v"(o[3][5]), "+v"(o[3][6]), "+v"(o[3][7]),
+                   [f] "=&v"(f), [t0] "=&v"(t0), [t1] "=&v"(t1), [t2] "=&v"(t2), [t3] "=&v"(t3)
+                 : [a] "v"(a), [own] "v"(own), [on] "s"(on)
                  : "memory", "scc");
 }
 
@@ -222,6 +242,16 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(2, 2)))
             }
         }
     }
+    // Else as many teams as the chunks leave room for, one workgroup for every chunk, that go through all sequences' tiles in step: a tile
+    // is read from memory once for all of its chunks then, and from the L2 by the others.  (Equal pieces of everything, where that would
+    // leave too many workgroups without work, each at a place of its own: the ragged batch of 16 sequences of 512 to 4096 keys, 15 chunks
+    // each, took 150 us, at 7 TB/s from behind the L2.)
+    bool in_step = false;
+    if (!aligned && p.chunks <= G) {
+        const int teams = G / p.chunks, of_team = max((total + teams - 1) / teams, least);
+        in_step = (int64_t)of_team * 4 <= (int64_t)per * 5;
+        if (in_step) per = of_team;
+    }
     // b, chunk: where the piece begins; tile: its first tile there; left: its tiles in all
     int b = -1, chunk = 0, tile = 0, left = 0, n_pieces = 1, number = 0, each = 0;
     if (aligned) {
@@ -244,21 +274,22 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(2, 2)))
             before = __builtin_amdgcn_readlane(last, 63);
         }
     } else {
-        const int64_t from = (int64_t)w * per, all = (int64_t)total * p.chunks;
+        const int64_t all = (int64_t)total * (in_step ? 1 : p.chunks), from = (int64_t)(in_step ? w / p.chunks : w) * per;
+        const int each_seq = in_step ? 1 : p.chunks;
         int64_t before = 0;
-        left = (int)min((int64_t)per, all - from);
+        left = (int)max((int64_t)0, min((int64_t)per, all - from));
         for (int b0 = 0; b0 < p.B && b < 0 && left > 0; b0 += 64) {
             const int t = tiles_at(b0), s = wave_scan(t, lane);
-            const uint64_t beyond = __builtin_amdgcn_ballot_w64(from < before + (int64_t)s * p.chunks);
+            const uint64_t beyond = __builtin_amdgcn_ballot_w64(from < before + (int64_t)s * each_seq);
             if (beyond) {
                 const int l = __builtin_ctzll(beyond);
                 b = b0 + l;
                 const int tiles = __builtin_amdgcn_readlane(t, l);
-                const int k = (int)(from - (before + (int64_t)(__builtin_amdgcn_readlane(s, l) - tiles) * p.chunks));
-                chunk = k / tiles;
-                tile = k - chunk * tiles;
+                const int k = (int)(from - (before + (int64_t)(__builtin_amdgcn_readlane(s, l) - tiles) * each_seq));
+                chunk = in_step ? w % p.chunks : k / tiles;
+                tile = in_step ? k : k - chunk * tiles;
             }
-            before += (int64_t)__builtin_amdgcn_readlane(s, 63) * p.chunks;
+            before += (int64_t)__builtin_amdgcn_readlane(s, 63) * each_seq;
         }
     }
     if (b < 0 || left <= 0) {
@@ -357,16 +388,17 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(2, 2)))
                 };
                 const u32x4_t flags = flagged(t - 1);                      // (looked at behind the products)
                 f32x4_t n[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
-                bf16x8_t kf[6];                                            // read six steps ahead
+                constexpr int AHEAD = 8;                                   // steps that key operands are read ahead
+                bf16x8_t kf[AHEAD];
 #pragma unroll
-                for (int ks = 0; ks < 6; ++ks) kf[ks] = key_of(ks);
+                for (int ks = 0; ks < AHEAD; ++ks) kf[ks] = key_of(ks);
                 __builtin_amdgcn_s_setprio(1);
 #pragma unroll
                 for (int ks = 0; ks < C::KS; ++ks) {
                     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                    for (int rg = 0; rg < 2; ++rg) mfma(n[rg], kf[ks % 6], q[rg][ks]);
-                    if (ks + 6 < C::KS) kf[ks % 6] = key_of(ks + 6);
+                    for (int rg = 0; rg < 2; ++rg) mfma(n[rg], kf[ks % AHEAD], q[rg][ks]);
+                    if (ks + AHEAD < C::KS) kf[ks % AHEAD] = key_of(ks + AHEAD);
                 }
                 __builtin_amdgcn_sched_barrier(0);
                 if (t > 0 && __builtin_expect(uniform((int)(flags[0] | flags[1] | flags[2] | flags[3])) != 0, 0)) outgrown(t - 1);
@@ -461,11 +493,15 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(2, 2)))
                     return __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
                 };
                 const u32x4_t flags = *(const u32x4_t *)(lds + C::FLAG_AT + ((t - 1) & 1) * 16);
-                bf16x8_t pf[4], vf[4];
+                constexpr int AHEAD = C::CB;                               // value operands read ahead
+                bf16x8_t pf[4], vf[AHEAD];
 #pragma unroll
                 for (int rg = 0; rg < 4; ++rg) pf[rg] = *(const bf16x8_t *)(lds + pb + rg * 16 * 64);
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int cb = 0; cb < 4; ++cb) vf[cb] = value_of(cb);
+                for (int cb = 0; cb < AHEAD; ++cb) vf[cb] = value_of(cb);
+                __builtin_amdgcn_sched_barrier(0);
+                asm volatile("" : "+v"(pf[0]), "+v"(pf[1]), "+v"(pf[2]), "+v"(pf[3]));       // (one wait for weights and flags)
                 const int on = uniform((int)(flags[0] | flags[1] | flags[2] | flags[3]));      // whether a reference was outgrown by that tile
                 if (__builtin_expect(on != 0, 0)) {
                     meet();
@@ -475,12 +511,7 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(2, 2)))
                 }
                 const int own = lds_at(lds + C::P_AT) + (t & 1) * C::P_BYTES + part * 1024 + anew(lane) * 16;      // (weights that are done with)
                 const int alpha = lds_at(lds + C::ALPHA_AT) + anew(col) * 4;
-#pragma unroll
-                for (int i = 0; i < 4 * C::CB; i += 8) {
-                    const int r0 = i / C::CB, r1 = (i + 4) / C::CB, c0 = i % C::CB, c1 = (i + 4) % C::CB;
-                    multiply(on, o[r0][c0], o[r0][c0 + 1], o[r0][c0 + 2], o[r0][c0 + 3], o[r1][c1], o[r1][c1 + 1], o[r1][c1 + 2], o[r1][c1 + 3], alpha + r0 * 64,
-                             alpha + r1 * 64, own);
-                }
+                multiply(t > 1 ? on : 0, o, alpha, own);                   // (before that it is zero)
                 if (on) meet();
                 const int next = t + 2, at = from + next, here = at < tree_tiles ? p.n - at * KEYS : len - (at - tree_tiles) * KEYS;
                 const unsigned char *src = at < tree_tiles ? nodes + (int64_t)at * C::TILE : past + (int64_t)(at - tree_tiles) * C::TILE;
@@ -492,8 +523,8 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(2, 2)))
 #pragma unroll
                 for (int cb = 0; cb < C::CB; ++cb) {
 #pragma unroll
-                    for (int rg = 0; rg < 4; ++rg) mfma(o[rg][cb], vf[cb % 4], pf[rg]);
-                    if (cb + 4 < C::CB) vf[cb % 4] = value_of(cb + 4);
+                    for (int rg = 0; rg < 4; ++rg) mfma(o[rg][cb], vf[cb % AHEAD], pf[rg]);
+                    if (cb + AHEAD < C::CB) vf[cb % AHEAD] = value_of(cb + AHEAD);
                     // (a load takes as long as the products of a block)
                     load_if<NT>(ask, src + cb * 128, load_at, dst + 8 * part * 128 + cb * C::PANEL);
                     if (cb == C::CB - 1) {
@@ -556,8 +587,8 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(2, 2)))
                         h.second = slot + h.stride;
                     } else {
                         h.pieces = 1 + (tiles - count + per - 1) / per;
-                        h.stride = 2;
-                        h.second = 2 * (w + 1);
+                        h.stride = in_step ? 2 * p.chunks : 2;
+                        h.second = 2 * w + h.stride;
                     }
                 }
                 p.header[w] = h;
@@ -565,9 +596,11 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(2, 2)))
             return;
         }
         tile = 0;
-        if (++chunk == p.chunks) {
+        if (in_step) {
+            ++b;
+        } else if (++chunk == p.chunks) {
             chunk = 0;
-            if (++b == p.B) return;
+            ++b;
         }
     }
 }
