@@ -37,6 +37,7 @@
 #include <type_traits>
 
 #include "fp4_format.h"
+#include "wave_ops.h"
 
 namespace {
 
@@ -277,37 +278,6 @@ __device__ __forceinline__ void absorb(f32x16_t (&sacc)[C::U], Block<C::D> &qs, 
     qs.l += sum;
 }
 
-// Inclusive sum and maximum over the wavefront's lanes (numbers >= 0).
-template <int CTRL, int ROWS>
-__device__ __forceinline__ int from_lane(int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false); }
-__device__ __forceinline__ int wave_scan(int v)
-{
-    v += from_lane<0x111, 0xf>(v);   // from 1, 2, 4, 8 lanes below within 16, then the sums of 16 and 32
-    v += from_lane<0x112, 0xf>(v);
-    v += from_lane<0x114, 0xf>(v);
-    v += from_lane<0x118, 0xf>(v);
-    v += from_lane<0x142, 0xa>(v);
-    v += from_lane<0x143, 0xc>(v);
-    return v;
-}
-__device__ __forceinline__ int wave_max(int v)
-{
-    v = max(v, from_lane<0x111, 0xf>(v));
-    v = max(v, from_lane<0x112, 0xf>(v));
-    v = max(v, from_lane<0x114, 0xf>(v));
-    v = max(v, from_lane<0x118, 0xf>(v));
-    v = max(v, from_lane<0x142, 0xa>(v));
-    v = max(v, from_lane<0x143, 0xc>(v));
-    return __builtin_amdgcn_readlane(v, 63);
-}
-__device__ __forceinline__ int wave_last(int v) { return __builtin_amdgcn_readlane(v, 63); }
-// n / d for 0 <= n < 2^30, d > 0 and a quotient below 2^20: rounded to 24 bits twice it is off by less than one.
-__device__ __forceinline__ int small_div(int n, int d)
-{
-    const int q = (int)((float)n * __builtin_amdgcn_rcpf((float)d)), r = n - q * d;
-    return q + (r >= d) - (r < 0);
-}
-__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
 template <int D, int QBP, bool NT>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void tree_attn_fp4_kernel(const Fp4AttnParams args)

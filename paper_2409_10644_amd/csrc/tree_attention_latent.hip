@@ -15,6 +15,7 @@
 #include <type_traits>
 
 #include "fp4_format.h"
+#include "wave_ops.h"
 
 namespace {
 
@@ -25,7 +26,7 @@ typedef __attribute__((ext_vector_type(4))) short s16x4_t;
 typedef __attribute__((ext_vector_type(4))) unsigned u32x4_t;
 typedef __attribute__((ext_vector_type(2))) unsigned u32x2_t;
 
-struct LatentHeader {                // what to fold: the unit that begins in a piece and goes on in others
+struct LatentHeader {                // what to fold: a unit (a chunk of a sequence) whose keys several workgroups shared
     int32_t pieces;                  // 0: none
     int32_t b, chunk;
     int32_t first, second, stride;   // slots of its parts: first, second, second + stride, ...
@@ -44,7 +45,7 @@ struct LatentParams {
     int32_t workgroups, slot_rows;
     RowDiv by_nrows;
     float c;                         // softmax scale * log2(e)
-    LatentHeader *header;            // [workgroups]
+    LatentHeader *header;            // [workgroups, or units where these are fewer]
     float *part_m, *part_l, *part_o; // slots of slot_rows rows: reference maximum (log2 units), sum, output
 };
 
@@ -57,7 +58,6 @@ constexpr int THREADS = 512;
 __device__ __align__(64) const unsigned char no_row[128] = {};
 
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
-__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 __device__ __forceinline__ const unsigned char *uniform(const unsigned char *a)
 {
     const uint64_t v = (uint64_t)a;
@@ -175,28 +175,6 @@ struct Cfg {
     static_assert(LDS <= 160 * 1024 && (DR == 64 || DR == 32), "");
 };
 
-__device__ __forceinline__ int wave_sum(int v)
-{
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) v += __shfl_xor(v, o);
-    return uniform(v);
-}
-__device__ __forceinline__ int wave_max(int v)
-{
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) v = max(v, __shfl_xor(v, o));
-    return uniform(v);
-}
-__device__ __forceinline__ int wave_scan(int v, int lane)        // inclusive
-{
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const int u = __shfl_up(v, o);
-        if (lane >= o) v += u;
-    }
-    return v;
-}
-
 template <int DL, int DR, bool NT>
 __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(2, 2))) void tree_attn_latent_kernel(const LatentParams args)
 {
@@ -209,15 +187,27 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(2, 2)))
     // Neighbours in the order of the work share an L2: the hardware deals workgroups to the eight dies in turn.
     const int w = (G & 7) == 0 ? ((int)blockIdx.x & 7) * (G >> 3) + ((int)blockIdx.x >> 3) : (int)blockIdx.x;
     const int tree_tiles = (p.n + KEYS - 1) / KEYS;
-    auto tiles_of = [&](int b) { return tree_tiles + (int)(((unsigned)min(max(p.lens[b], 0), p.max_prefix) + KEYS - 1) / KEYS); };
-
-    // ---- this workgroup's piece of the work
-    const int t_first = lane < p.B ? tiles_of(lane) : 0;
-    auto tiles_at = [&](int b0) { return b0 == 0 ? t_first : b0 + lane < p.B ? tiles_of(b0 + lane) : 0; };      // of sequence b0 + lane
+    // ---- this workgroup's piece of the work.  Lengths and places of 64 sequences, one per lane (in most calls all of them: one trip to
+    // memory).
+    int b_lanes = 0, len_l = 0;
+    int64_t base_l = 0;
+    auto fetch = [&](int b0) __attribute__((always_inline)) {
+        b_lanes = b0;
+        len_l = -1;
+        if (b0 + lane < p.B) {
+            len_l = min(max(p.lens[b0 + lane], 0), p.max_prefix);
+            base_l = p.seq_base[b0 + lane];
+        }
+    };
+    fetch(0);
+    auto tiles_at = [&](int b0) __attribute__((always_inline)) {           // of sequence b0 + lane
+        if (b0 != b_lanes) fetch(b0);
+        return len_l >= 0 ? tree_tiles + (int)(((unsigned)len_l + KEYS - 1) / KEYS) : 0;
+    };
     int total = 0, most = 0;
     for (int b0 = 0; b0 < p.B; b0 += 64) {
         const int t = tiles_at(b0);
-        total += wave_sum(t);
+        total += wave_last(wave_scan(t));
         most = max(most, wave_max(t));
     }
     const int pairs = p.B * p.chunks, least = max(MIN_TILES, (int)(0.5f * __builtin_amdgcn_sqrtf((float)most)));
@@ -228,7 +218,7 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(2, 2)))
         } else {
             auto fits = [&](int size) {
                 int sum = 0;
-                for (int b0 = 0; b0 < p.B; b0 += 64) sum += wave_sum((tiles_at(b0) + size - 1) / size);
+                for (int b0 = 0; b0 < p.B; b0 += 64) sum += wave_last(wave_scan(small_div(tiles_at(b0) + size - 1, size)));
                 return sum * p.chunks <= G;
             };
             int lo = per, hi = per + CROSS;
@@ -257,7 +247,7 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(2, 2)))
     if (aligned) {
         int before = 0;
         for (int b0 = 0; b0 < p.B && b < 0; b0 += 64) {
-            const int t = tiles_at(b0), e = (t + aligned - 1) / aligned, s = wave_scan(e * p.chunks, lane);
+            const int t = tiles_at(b0), e = small_div(t + aligned - 1, aligned), s = wave_scan(e * p.chunks);
             const int last = before + s;
             const uint64_t beyond = __builtin_amdgcn_ballot_w64(w < last);
             if (beyond) {
@@ -279,7 +269,7 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(2, 2)))
         int64_t before = 0;
         left = (int)max((int64_t)0, min((int64_t)per, all - from));
         for (int b0 = 0; b0 < p.B && b < 0 && left > 0; b0 += 64) {
-            const int t = tiles_at(b0), s = wave_scan(t, lane);
+            const int t = tiles_at(b0), s = wave_scan(t);
             const uint64_t beyond = __builtin_amdgcn_ballot_w64(from < before + (int64_t)s * each_seq);
             if (beyond) {
                 const int l = __builtin_ctzll(beyond);
@@ -293,7 +283,7 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(2, 2)))
         }
     }
     if (b < 0 || left <= 0) {
-        if (p.header && tid == 0) p.header[w].pieces = 0;
+        if (p.header && tid == 0 && pairs > G) p.header[w].pieces = 0;
         return;
     }
 
@@ -318,7 +308,8 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(2, 2)))
         chunk = uniform(chunk);
         tile = uniform(tile);
         left = uniform(left);
-        const int len = uniform(min(max(p.lens[b], 0), p.max_prefix)), tiles = tree_tiles + (int)(((unsigned)len + KEYS - 1) / KEYS);
+        if (b >= b_lanes + 64) fetch(b & ~63);
+        const int len = __builtin_amdgcn_readlane(len_l, b - b_lanes), tiles = tree_tiles + (int)(((unsigned)len + KEYS - 1) / KEYS);
         const int from = tile, count = min(left, tiles - tile);
         const bool whole = from == 0 && count == tiles, first = from == 0, last = from + count == tiles;
         const int slot = aligned ? 2 * w : 2 * w + (begun ? 1 : 0);
@@ -327,18 +318,23 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(2, 2)))
             // Query operands: rows col + 16 rg of this half of the chunk (behind the last: that one), channels 32 ks + 8 grp .. + 7.  And which
             // tree nodes the rows see among this lane's 4 keys: 4 bits per row and tree tile.
             bf16x8_t q[2][C::KS];
-            unsigned seen = 0;
+            uint64_t bits[2][2];
+            const uint16_t *src[2];
 #pragma unroll
             for (int rg = 0; rg < 2; ++rg) {
                 const int r = min(chunk * ROWS + 32 * rh + 16 * rg + col, p.rows - 1), h = row_div(r, p.by_nrows), i = p.row0 + r - h * (p.n - p.row0);
-                const uint16_t *src = p.q + (((int64_t)b * p.H + h) * p.node_stride + i) * C::D + 8 * grp;
-#pragma unroll
-                for (int ks = 0; ks < C::KS; ++ks) q[rg][ks] = *(const bf16x8_t *)(src + 32 * ks);
-                const uint64_t *bits = p.mask_bits + (int64_t)i * p.mask_words;
-                const int at = 16 * kg + 4 * grp;
-                seen |= (unsigned)((bits[0] >> at) & 15) << (4 * rg) | (unsigned)((bits[0] >> (at + 32)) & 15) << (8 + 4 * rg);
-                if (tree_tiles > 2) seen |= (unsigned)((bits[1] >> at) & 15) << (16 + 4 * rg) | (unsigned)((bits[1] >> (at + 32)) & 15) << (24 + 4 * rg);
+                src[rg] = p.q + (((int64_t)b * p.H + h) * p.node_stride + i) * C::D + 8 * grp;
+                const uint64_t *row = p.mask_bits + (int64_t)i * p.mask_words;
+                bits[rg][0] = row[0];
+                bits[rg][1] = tree_tiles > 2 ? row[1] : 0;
             }
+#pragma unroll
+            for (int rg = 0; rg < 2; ++rg)
+#pragma unroll
+                for (int ks = 0; ks < C::KS; ++ks) q[rg][ks] = *(const bf16x8_t *)(src[rg] + 32 * ks);
+            unsigned seen = 0;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) seen |= (unsigned)((bits[k & 1][k >> 2] >> (32 * (k >> 1 & 1) + 16 * kg + 4 * grp)) & 15) << (4 * k);      // tile k / 2, rows k % 2
             float ref[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, start[2] = {0.f, 0.f};      // (start: minus the reference, 0 while no key has been seen)
             f32x4_t s[2];
             // Of tile t, whose scores s holds: its maxima over all keys, new references, its weights again; what O^T has of the tiles before is
@@ -449,7 +445,8 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(2, 2)))
             }
             meet();
         } else {
-            const unsigned char *past = uniform((const unsigned char *)(p.cache + p.seq_base[b]));
+            const int64_t base = (int64_t)__builtin_amdgcn_readlane((int)(base_l >> 32), b - b_lanes) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)base_l, b - b_lanes);
+            const unsigned char *past = uniform((const unsigned char *)(p.cache + base));
             const unsigned char *nodes = uniform((const unsigned char *)(p.tree + (int64_t)b * p.node_stride * C::D));
             auto request = [&](int t) __attribute__((always_inline)) {     // tile t of this part, LOADS loads
                 const int at = from + t, here = at < tree_tiles ? p.n - at * KEYS : len - (at - tree_tiles) * KEYS;      // keys of the tile (or more)
@@ -574,27 +571,21 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(2, 2)))
         }
         left -= count;
         const bool more = !aligned && left > 0;
-        if (!more) {
-            if (p.header && tid == 0) {
-                LatentHeader h = {};
-                if (first && !last) {                                      // it begins here: who goes on with it
-                    h.b = b;
-                    h.chunk = chunk;
-                    h.first = slot;
-                    if (aligned) {
-                        h.pieces = n_pieces;
-                        h.stride = 2 * p.chunks;
-                        h.second = slot + h.stride;
-                    } else {
-                        h.pieces = 1 + (tiles - count + per - 1) / per;
-                        h.stride = in_step ? 2 * p.chunks : 2;
-                        h.second = 2 * w + h.stride;
-                    }
-                }
-                p.header[w] = h;
+        // What to fold: one word for every unit where no more of them than workgroups, else for every piece (only the last unit that begins
+        // in it can go on in others).
+        if (p.header && tid == 0 && (pairs <= G ? first : !more)) {
+            LatentHeader h = {};
+            if (first && !last) {                                          // it begins here: who goes on with it
+                h.b = b;
+                h.chunk = chunk;
+                h.first = slot;
+                h.stride = aligned || in_step ? 2 * p.chunks : 2;
+                h.second = 2 * w + h.stride;
+                h.pieces = aligned ? n_pieces : 1 + (tiles - count + per - 1) / per;
             }
-            return;
+            p.header[pairs <= G ? b * p.chunks + chunk : w] = h;
         }
+        if (!more) return;
         tile = 0;
         if (in_step) {
             ++b;
@@ -605,37 +596,47 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(2, 2)))
     }
 }
 
-// grid (pieces, slot_rows / 8): eight rows of the unit that begins in a piece, its parts added up in order.
+// grid (headers, slot_rows * DL / 1024): four channels of a row per thread, the unit's parts added up in order, eight of them asked for at
+// once (one after the other each is a trip to memory).
 template <int DL>
 __global__ __launch_bounds__(256) void tree_attn_latent_fold_kernel(const LatentParams p)
 {
     const LatentHeader h = p.header[blockIdx.x];
-    constexpr int PER = DL / 128;                    // pieces of four channels per thread
-    const int row = blockIdx.y * 8 + (threadIdx.x >> 5), r = h.chunk * ROWS + row, c = (threadIdx.x & 31) * 4;
+    constexpr int LANES = DL / 4;
+    const int row = blockIdx.y * (256 / LANES) + threadIdx.x / LANES, r = h.chunk * ROWS + row, c = threadIdx.x % LANES * 4;
     if (h.pieces == 0 || row >= p.slot_rows || r >= p.rows) return;
     float m = -INFINITY, sum = 0.f;
-    f32x4_t acc[PER];
+    f32x4_t acc = {0, 0, 0, 0};
+    for (int k0 = 0; k0 < h.pieces; k0 += 8) {
+        float pm[8], pl[8], now = m;
+        f32x4_t po[8];
 #pragma unroll
-    for (int x = 0; x < PER; ++x) acc[x] = (f32x4_t){0, 0, 0, 0};
-    for (int k = 0; k < h.pieces; ++k) {
-        const int64_t at = (int64_t)(k == 0 ? h.first : h.second + (k - 1) * h.stride) * p.slot_rows + row;
-        const float pm = p.part_m[at], pl = p.part_l[at], next = fmaxf(m, pm);
-        const float a = m == next ? 1.f : fast_exp2(m - next), e = pm == next ? 1.f : fast_exp2(pm - next);
-        m = next;
-        sum = sum * a + pl * e;
+        for (int i = 0; i < 8; ++i) {
+            const int k = min(k0 + i, h.pieces - 1);
+            const int64_t at = (int64_t)(k == 0 ? h.first : h.second + (k - 1) * h.stride) * p.slot_rows + row;
+            pm[i] = p.part_m[at];
+            pl[i] = p.part_l[at];
+            po[i] = *(const f32x4_t *)(p.part_o + at * DL + c);
+        }
 #pragma unroll
-        for (int x = 0; x < PER; ++x) acc[x] = acc[x] * a + *(const f32x4_t *)(p.part_o + at * DL + c + 128 * x) * e;
+        for (int i = 0; i < 8; ++i) now = fmaxf(now, pm[i]);
+        const float a = m == now ? 1.f : fast_exp2(m - now);               // (equal: also where no part has seen a key)
+        m = now;
+        sum *= a;
+        acc *= a;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (k0 + i >= h.pieces) break;
+            const float e = pm[i] == now ? 1.f : fast_exp2(pm[i] - now);
+            sum = fmaf(pl[i], e, sum);
+            acc += po[i] * e;
+        }
     }
     const int head = row_div(r, p.by_nrows), i = p.row0 + r - head * (p.n - p.row0);
-    uint16_t *dst = p.out + (((int64_t)h.b * p.H + head) * p.node_stride + i) * DL + c;
-    const float inv = 1.f / sum;
-#pragma unroll
-    for (int x = 0; x < PER; ++x) {
-        const f32x4_t y = acc[x] * inv;
-        const u32x2_t pk = {__builtin_bit_cast(unsigned, (bf16x2_t){(__bf16)y[0], (__bf16)y[1]}),
-                            __builtin_bit_cast(unsigned, (bf16x2_t){(__bf16)y[2], (__bf16)y[3]})};
-        *(u32x2_t *)(dst + 128 * x) = pk;
-    }
+    const f32x4_t y = acc * (1.f / sum);
+    const u32x2_t pk = {__builtin_bit_cast(unsigned, (bf16x2_t){(__bf16)y[0], (__bf16)y[1]}),
+                        __builtin_bit_cast(unsigned, (bf16x2_t){(__bf16)y[2], (__bf16)y[3]})};
+    *(u32x2_t *)(p.out + (((int64_t)h.b * p.H + head) * p.node_stride + i) * DL + c) = pk;
 }
 
 // ---------------------------------------------------------------------------------------------------- host
@@ -749,7 +750,9 @@ extern "C" int mcsd_tree_attention_latent(const mcsd_mask_view_t *mask, int32_t 
     if (hipGetLastError() != hipSuccess) return MCSD_EHIP;
     if (pl.bytes > 0) {
         auto fold = d_latent == 512 ? tree_attn_latent_fold_kernel<512> : tree_attn_latent_fold_kernel<256>;
-        mcsd_launch(MCSD_KERNEL_ATTN_MERGE, fold, dim3(pl.workgroups, (pl.slot_rows + 7) / 8), dim3(256), st, p);
+        const int64_t units = (int64_t)B * pl.chunks;
+        const unsigned headers = (unsigned)(units < pl.workgroups ? units : pl.workgroups), rows = 1024u / d_latent;
+        mcsd_launch(MCSD_KERNEL_ATTN_MERGE, fold, dim3(headers, (pl.slot_rows + rows - 1) / rows), dim3(256), st, p);
         return mcsd_hip_status(hipGetLastError());
     }
     return MCSD_OK;
