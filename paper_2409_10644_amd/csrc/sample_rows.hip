@@ -2,16 +2,18 @@
 //
 // A workgroup of 1024 threads has a row; it stays in its registers where it fits.  The tokens of a row are ordered by logit, largest
 // first, then by index; top-k, top-p and min-p each keep a beginning of that order, and the shortest counts.  Where it ends is found
-// without a sort: 2048 places for ranges of logits, the tokens of the one place where the count or the sum reaches its goal listed,
-// and each of them ranked against the others; more of them than the list holds are cut into 2048 ranges again, of logit and index as
-// one number.
+// without a sort.  For a top-k of up to half the threads: the k-th largest of the threads' own maxima is no more than the k-th largest
+// logit, so the few tokens from there on are listed and ranked against each other, and the rest of the call is about the list.
+// Otherwise: 2048 places for ranges of logits, the tokens of the one place where the count or the sum reaches its goal listed and ranked;
+// more of them than the list holds are cut into 2048 ranges again, of logit and index as one number.
 //
 // A weight is 2^((x - max) log2(e) / T) as a whole number of 2^-45: the sums are exact whatever their order (so atomics may add them),
 // a border of top-p and a draw depend on nothing but the weights, and 2^18 of them stay below 2^64.  It is computed in binary64,
-// so a border falls where 64 bits have it.  A probability is computed in fp32, of the exponent in two parts.
+// so a border falls where 64 bits have it.  Probabilities are computed in fp32, of a binary64 exponent.
 #include <math.h>
 
 #include "mcsd_internal.h"
+#include "wave_ops.h"
 
 namespace {
 
@@ -34,14 +36,22 @@ constexpr int THREADS = 1024, WAVES = 16, BINS = 2048, LIST = 1024, MAX_DRAW = 6
 constexpr int ONE = 45;                  // a weight of 1 is 2^45
 constexpr int FEW = 41;                  // distinct draws: below a sum of 2^41 the weights are made anew around the largest that is left
 constexpr int MAX_SEGMENTS = MCSD_MAX_VOCAB / 512;
+constexpr int HELD = 4, ROLL = HELD * THREADS;       // kept tokens in the order of indices: per thread, in all
 
+struct Ranked { u64 place, weight; };
 struct Shared {
-    u64 hist[BINS];
-    u64 list[LIST], weight[LIST];
+    union {
+        struct {
+            u64 hist[BINS];
+            Ranked list[LIST];
+        };
+        uint2 roll[ROLL];                // logit and index
+    };
     u64 segment[MAX_SEGMENTS];           // sums of 512 tokens
     u64 wave[WAVES], wave2[WAVES];
+    int32_t count[MAX_SEGMENTS];         // kept tokens of 512, then of all before them
     u64 above, sum, cut;
-    int32_t bin, listed, index, stop;
+    int32_t bin, listed, kept, winner;
     int32_t drawn[MAX_DRAW];
 };
 
@@ -54,10 +64,12 @@ __device__ __forceinline__ float of_ordered(unsigned k) { return __uint_as_float
 // Place in the order, the first has the largest.
 __device__ __forceinline__ u64 place_of(float x, int i) { return (u64)ordered(x) << 18 | (unsigned)(0x3ffff - i); }
 
+__device__ __forceinline__ int index_of(u64 place) { return 0x3ffff - (int)(place & 0x3ffff); }
+
 // 2^y for y <= 0: the polynomial is 2^f on [-1/2, 1/2] interpolated at the 11 Chebyshev points, off by at most 2^-51.5 of it.
 __device__ __forceinline__ u64 weight_of(double y)
 {
-    if (y < -(ONE + 1.0)) return 0;
+    y = fmax(y, -60.0);                                                    // (zero, without a branch)
     const double n = rint(y), f = y - n;
     double p = 0x1.e6063f7217bc6p-28;
     p = fma(p, f, 0x1.b675bca4eeebbp-24);
@@ -75,28 +87,33 @@ __device__ __forceinline__ u64 weight_of(double y)
     return __builtin_bit_cast(u64, s) & 0xfffffffffffffull;
 }
 
-__device__ __forceinline__ u64 shfl_xor64(u64 v, int o)
+// From other lanes of the wavefront, zero where there is none (see wave_ops.h for the steps).
+template <int CTRL, int ROWS>
+__device__ __forceinline__ u64 from_lane64(u64 v)
 {
-    return (u64)(unsigned)__shfl_xor((int)(v >> 32), o) << 32 | (unsigned)__shfl_xor((int)v, o);
+    return (u64)(unsigned)from_lane<CTRL, ROWS>((int)(v >> 32)) << 32 | (unsigned)from_lane<CTRL, ROWS>((int)v);
 }
-__device__ __forceinline__ u64 shfl_up64(u64 v, int o)
+__device__ __forceinline__ u64 wave_scan(u64 v)                            // inclusive
 {
-    return (u64)(unsigned)__shfl_up((int)(v >> 32), o) << 32 | (unsigned)__shfl_up((int)v, o);
-}
-__device__ __forceinline__ u64 wave_sum(u64 v)
-{
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) v += shfl_xor64(v, o);
+    v += from_lane64<0x111, 0xf>(v);
+    v += from_lane64<0x112, 0xf>(v);
+    v += from_lane64<0x114, 0xf>(v);
+    v += from_lane64<0x118, 0xf>(v);
+    v += from_lane64<0x142, 0xa>(v);
+    v += from_lane64<0x143, 0xc>(v);
     return v;
 }
-__device__ __forceinline__ u64 wave_scan(u64 v, int lane)                // inclusive
+__device__ __forceinline__ u64 lane_of(u64 v, int lane)
 {
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const u64 below = shfl_up64(v, o);
-        if (lane >= o) v += below;
-    }
-    return v;
+    return (u64)(unsigned)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 | (unsigned)__builtin_amdgcn_readlane((int)v, lane);
+}
+__device__ __forceinline__ u64 wave_sum(u64 v) { return lane_of(wave_scan(v), 63); }
+__device__ __forceinline__ u64 wave_largest(u64 v)
+{
+#define MCSD_STEP(CTRL, ROWS) { const u64 u = from_lane64<CTRL, ROWS>(v); v = u > v ? u : v; }
+    MCSD_STEP(0x111, 0xf) MCSD_STEP(0x112, 0xf) MCSD_STEP(0x114, 0xf) MCSD_STEP(0x118, 0xf) MCSD_STEP(0x142, 0xa) MCSD_STEP(0x143, 0xc)
+#undef MCSD_STEP
+    return lane_of(v, 63);
 }
 
 // Eight logits from index i on; behind the row's end minus infinity.  (Rows begin anywhere.)
@@ -148,19 +165,23 @@ __global__ __launch_bounds__(THREADS) void sample_rows_kernel(const SampleParams
 #pragma unroll
         for (int t = 0; t < NIT; ++t) kept_row[t].load(row, (t * THREADS + tid) * 8, V);
     }
-    // f(turn, first index, eight logits)
+    // f(turn, first index, eight logits); from memory four at a time
     auto each = [&](auto f) __attribute__((always_inline)) {
         if constexpr (NIT > 0) {
 #pragma unroll
             for (int t = 0; t < NIT; ++t) {
                 kept_row[t].anew();
                 if (t < turns) f(t, (t * THREADS + tid) * 8, kept_row[t]);
+                __builtin_amdgcn_sched_barrier(0);
             }
         } else {
-            for (int t = 0; t < turns; ++t) {
-                Eight<F32> x;
-                x.load(row, (t * THREADS + tid) * 8, V);
-                f(t, (t * THREADS + tid) * 8, x);
+            for (int t0 = 0; t0 < turns; t0 += 4) {
+                Eight<F32> x[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) x[k].load(row, ((t0 + k) * THREADS + tid) * 8, V);
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (t0 + k < turns) f(t0 + k, ((t0 + k) * THREADS + tid) * 8, x[k]);
             }
         }
     };
@@ -175,11 +196,7 @@ __global__ __launch_bounds__(THREADS) void sample_rows_kernel(const SampleParams
         return s;
     };
     auto block_max = [&](u64 v) {
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const u64 u = shfl_xor64(v, o);
-            v = u > v ? u : v;
-        }
+        v = wave_largest(v);
         __syncthreads();
         if (lane == 0) sh.wave[wave] = v;
         __syncthreads();
@@ -202,22 +219,16 @@ __global__ __launch_bounds__(THREADS) void sample_rows_kernel(const SampleParams
         }
     };
 
-    // ---- maximum, smallest finite logit, and whether the row is one
+    // ---- maximum (NaN where a logit is), and whether the row is a distribution
     const float T = p.s.temperature ? p.s.temperature[b] : 1.f, top_p = p.s.top_p ? p.s.top_p[b] : 1.f, min_p = p.s.min_p ? p.s.min_p[b] : 0.f;
     const int top_k = p.s.top_k ? p.s.top_k[b] : 0;
-    float mx = -INFINITY, mn = INFINITY;
-    bool bad = false;
-    each([&](int, int, const Eight<F32> &x) {
+    float own_max = -INFINITY;                                             // of the thread's logits
+    each([&](int, int, const Eight<F32> &x) __attribute__((always_inline)) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            mx = fmaxf(mx, x[k]);
-            mn = x[k] > -INFINITY ? fminf(mn, x[k]) : mn;
-            bad |= !(x[k] < INFINITY);                                     // NaN or infinite
-        }
+        for (int k = 0; k < 8; ++k) own_max = __builtin_elementwise_maximum(own_max, x[k]);
     });
-    bad = __syncthreads_or(bad) || !(T >= 0.f) || top_p != top_p || min_p != min_p;
-    mx = of_ordered((unsigned)block_max(ordered(mx)));
-    mn = of_ordered(~(unsigned)block_max(~ordered(mn)));
+    const bool bad = __syncthreads_or(!(own_max < INFINITY)) || !(T >= 0.f) || top_p != top_p || min_p != min_p;
+    const float mx = of_ordered((unsigned)block_max(ordered(own_max)));
     if (bad || mx == -INFINITY) {                                          // no distribution: NaN, or nothing to choose from: zeros
         const float v = bad ? NAN : 0.f;
         const float y[8] = {v, v, v, v, v, v, v, v};
@@ -229,74 +240,117 @@ __global__ __launch_bounds__(THREADS) void sample_rows_kernel(const SampleParams
     }
 
     // ---- the cut: a token is kept if its place is not below it, and its exponent not below min_y
-    const double c = T > 0.f ? 1.4426950408889634074 / (double)T : 0.0;
-    double top = (double)mx;                                               // what weights are relative to
+    const double c = T > 0.f ? 1.4426950408889634074 / (double)T : 0.0, mxd = (double)mx;
     const double min_y = min_p > 0.f ? fmin(log2((double)min_p), 0.0) : -INFINITY;
-    u64 cut = place_of(-INFINITY, 0) + 1;                                  // everything but minus infinity
-    // The place at which the sum of measure(logit) over the tokens from the first on reaches goal(sum of all) >= 1, which becomes the cut;
-    // returns the sum up to and with it.
-    auto find = [&](auto measure, auto goal) -> u64 {
-        const float range = fminf(mx - mn, 31.9f * T), scale = range > 0.f && range < INFINITY ? (BINS - 0.5f) / range : 0.f;
-        auto bin_of = [&](float x) { return scale > 0.f ? (int)fminf((mx - x) * scale, (float)(BINS - 1)) : 0; };
-        auto clear = [&]() {
-            sh.hist[tid] = 0;
-            sh.hist[tid + THREADS] = 0;
-            if (tid == 0) sh.listed = 0;
-            __syncthreads();
-        };
-        // where the sum of the 2048 places reaches the goal: sh.bin, and sh.above up to there; above: what is before the first of them
-        u64 target = 0;
-        auto choose = [&](u64 above, bool first) {
-            __syncthreads();
-            const u64 h0 = sh.hist[2 * tid], h1 = sh.hist[2 * tid + 1], in = wave_scan(h0 + h1, lane);
-            if (lane == 63) sh.wave2[wave] = in;
-            __syncthreads();
-            u64 before = above + in - (h0 + h1), all = above;
-            for (int k = 0; k < WAVES; ++k) {
-                all += sh.wave2[k];
-                if (k < wave) before += sh.wave2[k];
-            }
-            if (first) target = goal(all);
-            if (before < target && before + h0 >= target) { sh.bin = 2 * tid; sh.above = before; }
-            if (before + h0 < target && before + h0 + h1 >= target) { sh.bin = 2 * tid + 1; sh.above = before + h0; }
-            __syncthreads();
-        };
-        clear();
-        each([&](int, int i, const Eight<F32> &x) {
-#pragma unroll
-            for (int k = 0; k < 8; ++k)
-                if (place_of(x[k], i + k) >= cut) {
-                    const u64 m = measure(x[k]);
-                    if (m) atomicAdd(&sh.hist[bin_of(x[k])], m);
-                }
+    double top = mxd;                                                      // what weights are relative to
+    float cut_x = -3.402823466e38f;                                        // the cut's logit: of everything but minus infinity
+    int cut_i = 0;                                                         // and index; tokens of that logit are kept up to it, unless all are
+    bool all_equal_kept = true, by_min_p = false;
+    auto exponent = [&](float x) { return ((double)x - mxd) * c; };
+    auto weight = [&](float x) { return weight_of(((double)x - top) * c); };
+    auto kept = [&](float x, int i) __attribute__((always_inline)) {
+        const bool in = all_equal_kept ? x >= cut_x : x > cut_x || (x == cut_x && i <= cut_i);
+        return by_min_p ? in && exponent(x) >= min_y : in;
+    };
+    // each, but for wavefronts without a token from this logit on
+    auto max8 = [](const Eight<F32> &x) { return fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7]))); };
+    auto each_kept = [&](auto f, float from) __attribute__((always_inline)) {
+        each([&](int t, int i, const Eight<F32> &x) __attribute__((always_inline)) {
+            if (__builtin_amdgcn_ballot_w64(max8(x) >= from) != 0) f(t, i, x);
         });
-        choose(0, true);
-        int bin = sh.bin;
-        u64 above = sh.above, lo = 0, hi = ~0ull;
-        each([&](int, int i, const Eight<F32> &x) {
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const u64 at = place_of(x[k], i + k);
-                if (at >= cut && bin_of(x[k]) == bin) {
-                    const int n = atomicAdd(&sh.listed, 1);
-                    if (n < LIST) sh.list[n] = at;
-                }
-            }
-        });
+    };
+    auto set_cut = [&](u64 place, bool whole) {
+        cut_x = of_ordered((unsigned)(place >> 18));
+        cut_i = index_of(place);
+        all_equal_kept = whole;
+    };
+    auto clear = [&]() {
+        sh.hist[tid] = 0;
+        sh.hist[tid + THREADS] = 0;
+        if (tid == 0) sh.listed = 0;
         __syncthreads();
-        if (sh.listed > LIST) {
-            // from here on by place: the range lo .. hi is cut until its tokens fit the list
-            lo = ~0ull;
-            hi = 0;
-            each([&](int, int i, const Eight<F32> &x) {
+    };
+    // Where the sum over the 2048 places reaches goal(sum of all): sh.bin, and sh.above up to there; above: what is before the first of them.
+    u64 target = 0;
+    auto choose = [&](u64 above, auto goal) {
+        __syncthreads();
+        const u64 h0 = sh.hist[2 * tid], h1 = sh.hist[2 * tid + 1], in = wave_scan(h0 + h1);
+        if (lane == 63) sh.wave2[wave] = in;
+        __syncthreads();
+        u64 before = above + in - (h0 + h1), all = above;
+        for (int k = 0; k < WAVES; ++k) {
+            all += sh.wave2[k];
+            if (k < wave) before += sh.wave2[k];
+        }
+        target = goal(all);
+        if (before < target && before + h0 >= target) { sh.bin = 2 * tid; sh.above = before; }
+        if (before + h0 < target && before + h0 + h1 >= target) { sh.bin = 2 * tid + 1; sh.above = before + h0; }
+        __syncthreads();
+    };
+    auto append = [&](u64 place) __attribute__((always_inline)) {
+        const int n = atomicAdd(&sh.listed, 1);
+        if (n < LIST) sh.list[n].place = place;
+    };
+    // Every thread has one of the n listed tokens: its place (0: none), its measure, and that of all tokens before it in the order.
+    u64 mine = 0, own = 0, before_me = 0;
+    int rank_me = 0;
+    auto token_x = [&]() { return of_ordered((unsigned)(mine >> 18)); };
+    auto rank = [&](int n, u64 above, auto measure) {
+        mine = tid < n ? sh.list[tid].place : 0;
+        own = tid < n ? measure(token_x()) : 0;
+        if (tid < LIST) sh.list[tid] = Ranked{mine, own};                  // (behind the last: nothing, so that the loop below needs no end)
+        __syncthreads();
+        before_me = above;
+        rank_me = 0;
+        if (wave * 64 < n)
+            for (int o = 0; o < n; o += 8) {
+                Ranked r[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) r[k] = sh.list[o + k];
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
-                    const u64 at = place_of(x[k], i + k);
-                    if (at >= cut && bin_of(x[k]) == bin) {
+                    rank_me += r[k].place > mine;
+                    before_me += r[k].place > mine ? r[k].weight : 0;
+                }
+            }
+    };
+    // The place at which the sum of measure(logit) over the tokens from the first on reaches goal(sum of all) >= 1 becomes the cut; returns
+    // the sum up to and with it.
+    auto find = [&](auto measure, auto goal) -> u64 {
+        const float range = 31.9f * T, scale = range < INFINITY ? (BINS - 0.5f) / range : 0.f;      // (weights are zero beyond it)
+        auto bin_of = [&](float x) { return scale < INFINITY ? (int)fminf((mx - x) * scale, (float)(BINS - 1)) : 0; };
+        clear();
+        each_kept([&](int, int i, const Eight<F32> &x) __attribute__((always_inline)) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const u64 m = kept(x[k], i + k) ? measure(x[k]) : 0;
+                if (m) atomicAdd(&sh.hist[bin_of(x[k])], m);
+                if (k % 2) __builtin_amdgcn_sched_barrier(0);              // (not all eight at once: registers)
+            }
+        }, cut_x);
+        choose(0, goal);
+        const int bin = sh.bin;
+        u64 above = sh.above, lo = 0, hi = ~0ull;
+        each_kept([&](int, int i, const Eight<F32> &x) __attribute__((always_inline)) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (bin_of(x[k]) == bin && kept(x[k], i + k)) append(place_of(x[k], i + k));
+        }, cut_x);
+        __syncthreads();
+        bool parted = false;
+        if (sh.listed > LIST) {
+            // from here on by place: the range lo .. hi is cut until its tokens fit the list
+            parted = true;
+            lo = ~0ull;
+            hi = 0;
+            each([&](int, int i, const Eight<F32> &x) __attribute__((always_inline)) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (bin_of(x[k]) == bin && kept(x[k], i + k)) {
+                        const u64 at = place_of(x[k], i + k);
                         lo = at < lo ? at : lo;
                         hi = at > hi ? at : hi;
                     }
-                }
             });
             hi = block_max(hi);
             lo = ~block_max(~lo);
@@ -305,7 +359,7 @@ __global__ __launch_bounds__(THREADS) void sample_rows_kernel(const SampleParams
                 while ((hi - lo) >> shift >= BINS) ++shift;
                 __syncthreads();
                 clear();
-                each([&](int, int i, const Eight<F32> &x) {
+                each([&](int, int i, const Eight<F32> &x) __attribute__((always_inline)) {
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {
                         const u64 at = place_of(x[k], i + k);
@@ -315,109 +369,325 @@ __global__ __launch_bounds__(THREADS) void sample_rows_kernel(const SampleParams
                         }
                     }
                 });
-                choose(above, false);
+                choose(above, [&](u64) { return target; });
                 above = sh.above;
                 const u64 end = hi - ((u64)sh.bin << shift), begin = end - ((1ull << shift) - 1);
                 hi = end;
                 lo = begin > lo && begin <= end ? begin : lo;
-                each([&](int, int i, const Eight<F32> &x) {
+                each([&](int, int i, const Eight<F32> &x) __attribute__((always_inline)) {
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {
                         const u64 at = place_of(x[k], i + k);
-                        if (at >= lo && at <= hi) {
-                            const int n = atomicAdd(&sh.listed, 1);
-                            if (n < LIST) sh.list[n] = at;
-                        }
+                        if (at >= lo && at <= hi) append(at);
                     }
                 });
                 __syncthreads();
             }
         }
-        // the listed ones among themselves
-        const int n = sh.listed;
-        u64 mine = 0, own = 0;
-        if (tid < n) {
-            mine = sh.list[tid];
-            own = measure(of_ordered((unsigned)(mine >> 18)));
-            sh.weight[tid] = own;
-        }
+        rank(sh.listed, above, measure);
+        if (mine && before_me < target && before_me + own >= target) { sh.cut = mine; sh.sum = before_me + own; }
         __syncthreads();
-        if (tid < n) {
-            u64 before = above;
-            for (int k = 0; k < n; ++k) before += sh.list[k] > mine ? sh.weight[k] : 0;
-            if (before < target && before + own >= target) { sh.cut = mine; sh.sum = before + own; }
-        }
-        __syncthreads();
-        cut = sh.cut;
+        const u64 place = sh.cut;
+        set_cut(place, !__syncthreads_or(parted || (mine && mine >> 18 == place >> 18 && mine < place)));
         return sh.sum;
     };
-    auto weight = [&](float x) { return weight_of(((double)x - top) * c); };
+    auto share = [&](u64 all) { const double g = ceil((double)top_p * (double)all); return g < 1.0 ? (u64)1 : (u64)g; };      // of the sum, to top-p
+
+    // Of the n listed tokens, all from the first on down to somewhere behind what is kept: what top-k, top-p and min-p leave.
+    u64 sum = 0;
+    bool exact = false;                                                    // whether that is the sum of what is kept
+    auto settle = [&](int n, int k) {
+        rank(n, 0, weight);
+        if (mine && rank_me == min(k, n) - 1) sh.sum = before_me + own;
+        __syncthreads();
+        const u64 goal = share(sh.sum);
+        const bool in = mine && rank_me < k && (top_p >= 1.f || before_me < goal) && exponent(token_x()) >= min_y;
+        const int m = __syncthreads_count(in);
+        if (in && rank_me == m - 1) { sh.cut = mine; sh.sum = before_me + own; }
+        __syncthreads();
+        const u64 place = sh.cut;
+        sum = sh.sum;
+        exact = true;
+        set_cut(place, !__syncthreads_or(mine && mine >> 18 == place >> 18 && mine < place));
+    };
     if (T == 0.f || top_k == 1) {                                          // the largest alone
         int first = V;
-        each([&](int, int i, const Eight<F32> &x) {
+        each_kept([&](int, int i, const Eight<F32> &x) __attribute__((always_inline)) {
 #pragma unroll
             for (int k = 7; k >= 0; --k) first = x[k] == mx && i + k < first ? i + k : first;
-        });
-        cut = place_of(mx, (int)~block_max(~(u64)(unsigned)first));
+        }, mx);
+        first = (int)~block_max(~(u64)(unsigned)first);
+        set_cut(place_of(mx, first), false);
+        sum = 1ull << ONE;
+        exact = true;
     } else {
-        if (top_k > 0 && top_k < V)
-            find([](float) { return (u64)1; }, [&](u64 all) { return all < (u64)top_k ? all : (u64)top_k; });
-        if (top_p < 1.f)
-            find([&](float x) { return weight(x); },
-                 [&](u64 all) { const double g = ceil((double)top_p * (double)all); return g < 1.0 ? (u64)1 : (u64)g; });
+        const bool some = top_k > 0 && top_k < V;
+        if (some && top_k <= THREADS / 2) {
+            // the threads' maxima by ranges of their own, the range in which the k-th of them is, and all tokens down to its end
+            const float low = of_ordered(~(unsigned)block_max(own_max > -INFINITY ? ~ordered(own_max) : 0u));
+            const float range = mx - low, scale = range > 0.f && range < INFINITY ? (BINS - 0.5f) / range : 0.f;
+            auto bin_of = [&](float x) { return scale < INFINITY ? (int)fminf((mx - x) * scale, (float)(BINS - 1)) : 0; };
+            clear();
+            if (own_max > -INFINITY) atomicAdd(&sh.hist[bin_of(own_max)], (u64)1);
+            choose(0, [&](u64 all) { return all < (u64)top_k ? all : (u64)top_k; });
+            const int bin = target < (u64)top_k ? BINS : sh.bin;           // (fewer threads with tokens than top_k: all tokens)
+            auto wanted = [&](float x) { return x >= cut_x && (x >= low ? bin_of(x) <= bin : bin == BINS); };
+            each([&](int, int i, const Eight<F32> &x) __attribute__((always_inline)) {
+                if (__builtin_amdgcn_ballot_w64(wanted(max8(x))) == 0) return;
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (wanted(x[k])) append(place_of(x[k], i + k));
+            });
+            __syncthreads();
+            const int n = sh.listed;
+            __syncthreads();
+            if (n <= LIST) settle(n, top_k);
+        }
+        if (!exact) {
+            if (some) find([](float) { return (u64)1; }, [&](u64 all) { return all < (u64)top_k ? all : (u64)top_k; });
+            if (top_p < 1.f) {
+                sum = find(weight, share);
+                exact = !(min_p > 0.f);
+            }
+            by_min_p = min_p > 0.f;
+        }
     }
-    auto exponent = [&](float x) { return ((double)x - (double)mx) * c; };
-    auto kept = [&](float x, int i) { return place_of(x, i) >= cut && exponent(x) >= min_y; };
-    auto drawn_before = [&](int i, int n) {
-        bool is = false;
-        for (int k = 0; k < n; ++k) is |= sh.drawn[k] == i;
+
+    // ---- sum of the kept weights: exactly where something is drawn, of all but the first `without` drawn tokens, and of every segment
+    auto drawn_of = [&](int i, int n) {                                    // which of the eight tokens from i on are among the first n drawn
+        unsigned is = 0;
+        for (int d = 0; d < n; ++d) {
+            const unsigned k = (unsigned)(sh.drawn[d] - i);
+            is |= k < 8 ? 1u << k : 0;
+        }
         return is;
     };
-
-    // ---- sum, probabilities
-    // (all but the first `without` drawn tokens; also of every segment, where there is something to draw)
     auto sum_up = [&](int without) {
         u64 part = 0;
-        each([&](int t, int i, const Eight<F32> &x) {
+        for (int s = tid; s < turns * WAVES; s += THREADS) sh.segment[s] = 0;
+        __syncthreads();
+        each_kept([&](int t, int i, const Eight<F32> &x) __attribute__((always_inline)) {
+            const unsigned drawn = drawn_of(i, without);
             u64 here = 0;
 #pragma unroll
-            for (int k = 0; k < 8; ++k)
-                if (kept(x[k], i + k) && !drawn_before(i + k, without)) here += weight(x[k]);
-            if (p.n_draw) {
-                const u64 s = wave_sum(here);
-                if (lane == 0) sh.segment[t * WAVES + wave] = s;
+            for (int k = 0; k < 8; ++k) {
+                here += kept(x[k], i + k) && !(drawn >> k & 1) ? weight(x[k]) : 0;
+                if (k % 2) __builtin_amdgcn_sched_barrier(0);
             }
+            const u64 s = wave_sum(here);
+            if (lane == 0) sh.segment[t * WAVES + wave] = s;
             part += here;
-        });
+        }, cut_x);
         return block_sum(part);
     };
-    u64 sum = sum_up(0);
-    if (probs) {
-        const float inv = (float)(0x1p45 / (double)sum);
-        each([&](int, int i, const Eight<F32> &x) {
-            float y[8];
+    // Weights in fp32: the difference and its product with log2(e) / T in two parts each, the second of which multiplies the exponential.
+    // (By way of binary64 its conversions cost most: 110 cycles of a SIMD per 64 tokens, so 60.  That way is for what fp32 does not hold.)
+    const float c_hi = (float)c, c_lo = (float)(c - (double)c_hi);
+    const bool beyond = !(c < 1e30) || mx > 1e37f;
+    auto powers = [&](const Eight<F32> &x, float (&e)[8]) __attribute__((always_inline)) {
+        if (__builtin_expect(beyond, 0)) {
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-                const double e = fmax(exponent(x[k]), -200.0);             // (nothing in fp32 either way; masks are as low as -3.4e38)
-                const float hi = (float)e, lo = (float)(e - (double)hi);
-                y[k] = kept(x[k], i + k) ? __builtin_amdgcn_exp2f(hi) * inv * fmaf(lo, 0.69314718f, 1.f) : 0.f;
+                const double y = fmax(exponent(x[k]), -1000.0), whole = rint(y);
+                e[k] = __builtin_amdgcn_ldexpf(__builtin_amdgcn_exp2f((float)(y - whole)), (int)whole);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            return;
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const float d = x[k] - mx, back = d + mx, lost = (x[k] - back) + ((back - d) - mx);      // x - mx = d + lost
+            const float y = d * c_hi, rest = fmaf(lost, c_hi, fmaf(d, c_lo, fmaf(d, c_hi, -y))), w = __builtin_amdgcn_exp2f(y);
+            e[k] = y > -150.f ? fmaf(w * rest, 0.69314718f, w) : 0.f;      // (masks are as low as -3.4e38)
+            if (k % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    float inv = 0.f;
+    if (exact || p.n_draw) {
+        if (!exact) sum = 0;
+    } else {
+        double part = 0.0;
+        each([&](int, int i, const Eight<F32> &x) __attribute__((always_inline)) {
+            float e[8];
+            powers(x, e);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) e[k] = kept(x[k], i + k) ? e[k] : 0.f;
+            part += (double)(((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7])));
+        });
+        // (in the order of the lanes and wavefronts: the same every time)
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) part += __shfl_xor(part, o);
+        __syncthreads();
+        if (lane == 0) sh.wave[wave] = __builtin_bit_cast(u64, part);
+        __syncthreads();
+        double all = 0.0;
+        for (int k = 0; k < WAVES; ++k) all += __builtin_bit_cast(double, sh.wave[k]);
+        inv = (float)(1.0 / all);
+    }
+
+    // ---- what draws are made from: the kept tokens in the order of indices, HELD of them in every thread, with their weights and those of
+    // all before; or, where they are too many, sums of segments of 512
+    float roll_x[HELD];
+    int roll_i[HELD], alive = 0;                                           // (which of them are there and not drawn: bits)
+    u64 roll_w[HELD], before_roll = 0;
+    bool rolled = false;
+    // weights relative to `top`, their sums before every thread and of all
+    auto weigh_roll = [&]() {
+        u64 here = 0;
+#pragma unroll
+        for (int k = 0; k < HELD; ++k) {
+            roll_w[k] = alive >> k & 1 ? weight(roll_x[k]) : 0;
+            here += roll_w[k];
+        }
+        const u64 in = wave_scan(here);
+        __syncthreads();
+        if (lane == 63) sh.wave[wave] = in;
+        __syncthreads();
+        before_roll = in - here;
+        sum = 0;
+        for (int k = 0; k < WAVES; ++k) {
+            if (k < wave) before_roll += sh.wave[k];
+            sum += sh.wave[k];
+        }
+    };
+    if (p.n_draw) {
+        const int segments = turns * WAVES;
+        for (int s = tid; s < segments; s += THREADS) sh.count[s] = 0;
+        __syncthreads();
+        each_kept([&](int t, int i, const Eight<F32> &x) __attribute__((always_inline)) {
+            int here = 0;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) here += kept(x[k], i + k);
+            const int all = ::wave_last(::wave_scan(here));
+            if (lane == 0) sh.count[t * WAVES + wave] = all;
+        }, cut_x);
+        __syncthreads();
+        if (wave == 0) {                                                   // eight segments a lane
+            int mine8[MAX_SEGMENTS / 64], all = 0;
+#pragma unroll
+            for (int k = 0; k < MAX_SEGMENTS / 64; ++k) {
+                const int s = lane * (MAX_SEGMENTS / 64) + k;
+                mine8[k] = all;
+                all += s < segments ? sh.count[s] : 0;
+            }
+            const int in = ::wave_scan(all);
+            if (lane == 63) sh.kept = in;
+#pragma unroll
+            for (int k = 0; k < MAX_SEGMENTS / 64; ++k)
+                if (lane * (MAX_SEGMENTS / 64) + k < segments) sh.count[lane * (MAX_SEGMENTS / 64) + k] = in - all + mine8[k];
+        }
+        __syncthreads();
+        if (sh.kept <= ROLL) {
+            rolled = true;
+            each_kept([&](int t, int i, const Eight<F32> &x) __attribute__((always_inline)) {
+                int here = 0;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) here += kept(x[k], i + k);
+                int at = sh.count[t * WAVES + wave] + ::wave_scan(here) - here;
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (kept(x[k], i + k)) sh.roll[at++] = make_uint2(__float_as_uint(x[k]), i + k);
+            }, cut_x);
+            __syncthreads();
+#pragma unroll
+            for (int k = 0; k < HELD; ++k) {
+                const uint2 v = sh.roll[tid * HELD + k];
+                roll_x[k] = __uint_as_float(v.x);
+                roll_i[k] = (int)v.y;
+                alive |= tid * HELD + k < sh.kept ? 1 << k : 0;
+            }
+            weigh_roll();
+        } else {
+            sum = sum_up(0);
+        }
+    }
+    if (exact || p.n_draw) inv = (float)(0x1p45 / (double)sum);
+
+    // ---- probabilities
+    if (probs) {
+        each([&](int, int i, const Eight<F32> &x) __attribute__((always_inline)) {
+            float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+            if (__builtin_amdgcn_ballot_w64(max8(x) >= cut_x) != 0) {      // (the other wavefronts have zeros to write)
+                powers(x, y);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) y[k] = kept(x[k], i + k) ? y[k] * inv : 0.f;
             }
             if (i < V) write8(i, y);
         });
     }
+    if (!p.n_draw) return;
 
     // ---- draws: the first token, in the order of indices, at which the sum of the weights exceeds u times all of it
+    auto goal_of = [&](float u) {
+        u = fminf(fmaxf(u, 0.f), 0x1.fffffep-1f);
+        const u64 goal = (u64)((double)u * (double)sum);
+        return goal < sum ? goal : sum - 1;
+    };
+    if (rolled) {
+        // the thread that has it: which of its tokens
+        auto take = [&](u64 goal) {
+            int who = -1;
+            u64 before = before_roll;
+#pragma unroll
+            for (int k = 0; k < HELD; ++k) {
+                if (before <= goal && before + roll_w[k] > goal) who = k;
+                before += roll_w[k];
+            }
+            return who;
+        };
+        for (int d = 0; d < p.n_draw; ++d) {
+            if (p.distinct && d && sum < 1ull << FEW) {                    // (the same for all threads)
+                u64 best = 0;                                              // the largest that is left, and all weights relative to it
+#pragma unroll
+                for (int k = 0; k < HELD; ++k)
+                    if (alive >> k & 1) {
+                        const u64 at = place_of(roll_x[k], roll_i[k]);
+                        best = at > best ? at : best;
+                    }
+                best = block_max(best);
+                if (best == 0) {                                           // nothing is left
+                    if (tid >= d && tid < p.n_draw) tokens[tid] = -1;
+                    return;
+                }
+                top = (double)of_ordered((unsigned)(best >> 18));
+                weigh_roll();
+            }
+            const u64 goal = goal_of(us[d]);
+            const int who = take(goal);
+            if (who >= 0) {
+                int token = 0;
+                u64 weighs = 0;
+#pragma unroll
+                for (int k = 0; k < HELD; ++k)
+                    if (who == k) {
+                        token = roll_i[k];
+                        weighs = roll_w[k];
+                        if (p.distinct) roll_w[k] = 0;
+                    }
+                tokens[d] = token;
+                if (p.distinct) {
+                    alive &= ~(1 << who);
+                    sh.winner = tid;
+                    sh.above = weighs;
+                }
+            }
+            if (p.distinct) {
+                __syncthreads();
+                if (tid > sh.winner) before_roll -= sh.above;
+                sum -= sh.above;
+                __syncthreads();
+            }
+        }
+        return;
+    }
     const int segments = turns * WAVES;
     // by one wavefront: the token, and what it weighs
     auto draw = [&](float u, int without, u64 &weighs) {
-        u = fminf(fmaxf(u, 0.f), 0x1.fffffep-1f);
-        u64 goal = (u64)((double)u * (double)sum);
-        goal = goal < sum ? goal : sum - 1;
-        u64 own = 0;
+        u64 goal = goal_of(u), here = 0;
         constexpr int PER = MAX_SEGMENTS / 64;
         const int s0 = lane * PER;
-        for (int k = 0; k < PER; ++k) own += s0 + k < segments ? sh.segment[s0 + k] : 0;
-        u64 in = wave_scan(own, lane), before = in - own;
+        for (int k = 0; k < PER; ++k) here += s0 + k < segments ? sh.segment[s0 + k] : 0;
+        u64 in = wave_scan(here), before = in - here;
         int s = -1;
         if (before <= goal && in > goal) {
             s = s0;
@@ -429,15 +699,17 @@ __global__ __launch_bounds__(THREADS) void sample_rows_kernel(const SampleParams
         const int i = (s * 64 + lane) * 8;
         Eight<F32> x;
         x.load(row, i, V);
+        const unsigned drawn = drawn_of(i, without);
         u64 w[8];
-        own = 0;
+        here = 0;
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-            w[k] = kept(x[k], i + k) && !drawn_before(i + k, without) ? weight(x[k]) : 0;
-            own += w[k];
+            w[k] = kept(x[k], i + k) && !(drawn >> k & 1) ? weight(x[k]) : 0;
+            here += w[k];
+            __builtin_amdgcn_sched_barrier(0);
         }
-        in = wave_scan(own, lane);
-        before = in - own;
+        in = wave_scan(here);
+        before = in - here;
         int token = -1;
         weighs = 0;
         if (before <= goal && in > goal) {
@@ -454,7 +726,6 @@ __global__ __launch_bounds__(THREADS) void sample_rows_kernel(const SampleParams
         weighs = (u64)(unsigned)__shfl((int)(weighs >> 32), who) << 32 | (unsigned)__shfl((int)weighs, who);
         return __shfl(token, who);
     };
-    if (!p.n_draw) return;
     __syncthreads();
     if (!p.distinct) {
         for (int d = wave; d < p.n_draw; d += WAVES) {
@@ -466,15 +737,15 @@ __global__ __launch_bounds__(THREADS) void sample_rows_kernel(const SampleParams
     }
     for (int d = 0; d < p.n_draw; ++d) {
         if (d && sum < 1ull << FEW) {                                      // (the same for all threads)
-            // the largest that is left, and all weights relative to it
             u64 best = 0;
-            each([&](int, int i, const Eight<F32> &x) {
+            each_kept([&](int, int i, const Eight<F32> &x) __attribute__((always_inline)) {
+                const unsigned drawn = drawn_of(i, d);
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
                     const u64 at = place_of(x[k], i + k);
-                    if (at > best && kept(x[k], i + k) && !drawn_before(i + k, d)) best = at;
+                    if (at > best && kept(x[k], i + k) && !(drawn >> k & 1)) best = at;
                 }
-            });
+            }, cut_x);
             best = block_max(best);
             if (best == 0) {                                               // nothing is left
                 if (tid >= d && tid < p.n_draw) tokens[tid] = -1;
