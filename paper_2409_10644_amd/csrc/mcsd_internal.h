@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 #include <hip/hip_ext.h>
 #include <stdint.h>
+#include <atomic>
 #include "mcsd.h"
 
 struct mcsd_mask {
@@ -33,6 +34,22 @@ constexpr int64_t MCSD_MAX_GRID_256 = 0xffffff;
 constexpr int64_t MCSD_MAX_GRID_1024 = 0x3fffff;
 
 static inline int mcsd_hip_status(hipError_t e) { return e == hipSuccess ? MCSD_OK : MCSD_EHIP; }
+// Of the current device, for grids that are sized by it.
+inline int mcsd_compute_units()
+{
+    static std::atomic<int> cus_of_device[64];
+    int dev = 0;
+    if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) {
+        (void)hipGetLastError();
+        return 256;                  // no device to ask: the whole chip
+    }
+    int v = cus_of_device[dev].load(std::memory_order_relaxed);
+    if (v == 0) {
+        if (hipDeviceGetAttribute(&v, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || v < 1) v = 256;
+        cus_of_device[dev].store(v, std::memory_order_relaxed);
+    }
+    return v;
+}
 
 // Accelerator dies (each with its own L2) of `device` when the hardware deals workgroup i of a launch to die
 // i % dies, as established by a probe launch in mcsd_build_mask; 0 when unknown or not so.  Defined in mask.cpp.
@@ -41,7 +58,6 @@ int mcsd_xcc_count(int device);
 // One-shot profiling events per kernel (see mcsd_profile_next); defined in mask.cpp.  Arming stores `stop` and then
 // `start`; a launch takes `start` with an atomic exchange, so exactly one launch consumes an armed pair even when
 // several host threads launch the same kernel at once.
-#include <atomic>
 struct McsdProfileSlot { std::atomic<hipEvent_t> start, stop; };
 extern McsdProfileSlot g_mcsd_profile[6];
 

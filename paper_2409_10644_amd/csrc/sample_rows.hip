@@ -1,15 +1,21 @@
 // From logits to the probability rows that the verification takes, and tokens drawn from them (definition in mcsd.h).
 //
-// A workgroup of 1024 threads has a row; it stays in its registers where it fits.  The tokens of a row are ordered by logit, largest
-// first, then by index; top-k, top-p and min-p each keep a beginning of that order, and the shortest counts.  Where it ends is found
-// without a sort.  For a top-k of up to half the threads: the k-th largest of the threads' own maxima is no more than the k-th largest
-// logit, so the few tokens from there on are listed and ranked against each other, and the rest of the call is about the list.
-// Otherwise: 2048 places for ranges of logits, the tokens of the one place where the count or the sum reaches its goal listed and ranked;
-// more of them than the list holds are cut into 2048 ranges again, of logit and index as one number.
+// A workgroup has a row and reads it once per pass, from memory the first time and from the L2 after it.  The tokens of a row are ordered
+// by logit, largest first, then by index; top-k, top-p and min-p each keep a beginning of that order, and the shortest counts.  Where it
+// ends is found without a sort.  For a top-k of up to half the threads: the k-th largest of the threads' own maxima is no more than the
+// k-th largest logit, so the few tokens from there on are listed and ranked against each other, and the rest of the call is about the
+// list.  Otherwise: two places per thread for ranges of logits, the tokens of the one place where the count or the sum reaches its goal
+// listed and ranked; more of them than the list holds are cut into as many ranges again, of logit and index as one number.
 //
 // A weight is 2^((x - max) log2(e) / T) as a whole number of 2^-45: the sums are exact whatever their order (so atomics may add them),
 // a border of top-p and a draw depend on nothing but the weights, and 2^18 of them stay below 2^64.  It is computed in binary64,
-// so a border falls where 64 bits have it.  Probabilities are computed in fp32, of a binary64 exponent.
+// so a border falls where 64 bits have it.  Probabilities are computed in fp32 pairs, or of a binary64 exponent.
+//
+// What bounds it, at 32000 logits a row: few rows, the passes and meetings of one workgroup one after the other (45 rows of bf16, top-k 50
+// with top-p and min-p: 22 us; 64 rows of fp32 with top-p and four distinct draws: 50 us; 32 rows of 131077, mixed: 157 us, most of it
+// the binary64 weights of the rows with a top-p alone); many rows, the exponentials, made once for the sum and once for the row
+// (2816 rows of bf16: 187 us for 541 MB, 2.9 TB/s; kept between the two they would need the LDS that the second workgroup has).
+// Rows in LDS between the passes took 24 / 70 / - / 276 us for these four, two rows requested ahead more 22.6 / 57 / 166 / 187.
 #include <math.h>
 
 #include "mcsd_internal.h"
@@ -32,23 +38,24 @@ struct SampleParams {
     int64_t t_batch;
 };
 
-constexpr int THREADS = 1024, WAVES = 16, BINS = 2048, LIST = 1024, MAX_DRAW = 64;
+constexpr int MAX_DRAW = 64;
 constexpr int ONE = 45;                  // a weight of 1 is 2^45
 constexpr int FEW = 41;                  // distinct draws: below a sum of 2^41 the weights are made anew around the largest that is left
 constexpr int MAX_SEGMENTS = MCSD_MAX_VOCAB / 512;
-constexpr int HELD = 4, ROLL = HELD * THREADS;       // kept tokens in the order of indices: per thread, in all
+constexpr int HELD = 4;                  // kept tokens in the order of indices per thread
 
 struct Ranked { u64 place, weight; };
+template <int THREADS>
 struct Shared {
     union {
         struct {
-            u64 hist[BINS];
-            Ranked list[LIST];
+            u64 hist[2 * THREADS];
+            Ranked list[THREADS];
         };
-        uint2 roll[ROLL];                // logit and index
+        uint2 roll[HELD * THREADS];      // logit and index
     };
     u64 segment[MAX_SEGMENTS];           // sums of 512 tokens
-    u64 wave[WAVES], wave2[WAVES];
+    u64 wave[THREADS / 64];
     int32_t count[MAX_SEGMENTS];         // kept tokens of 512, then of all before them
     u64 above, sum, cut;
     int32_t bin, listed, kept, winner;
@@ -118,7 +125,7 @@ __device__ __forceinline__ u64 wave_largest(u64 v)
 
 // Eight logits from index i on; behind the row's end minus infinity.  (Rows begin anywhere.)
 template <bool F32>
-struct Eight {
+struct __attribute__((aligned(16))) Eight {
     unsigned w[F32 ? 8 : 4];
     __device__ __forceinline__ void load(const void *row, int i, int V)
     {
@@ -139,12 +146,6 @@ struct Eight {
             }
         }
     }
-    // What one pass makes of them is not kept in registers for the next.
-    __device__ __forceinline__ void anew()
-    {
-#pragma unroll
-        for (int k = 0; k < (F32 ? 8 : 4); ++k) asm volatile("" : "+v"(w[k]));
-    }
     __device__ __forceinline__ float operator[](int k) const
     {
         if constexpr (F32) return __uint_as_float(w[k]);
@@ -152,37 +153,28 @@ struct Eight {
     }
 };
 
-// NIT: turns of 8192 logits that the registers hold; 0: the row is read again for every pass
-template <bool F32, int NIT>
-__global__ __launch_bounds__(THREADS) void sample_rows_kernel(const SampleParams p)
+template <bool F32, int THREADS>
+__global__ __launch_bounds__(THREADS, 4) void sample_rows_kernel(const SampleParams p)
 {
-    __shared__ Shared sh;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = blockIdx.x, b = blockIdx.y;
-    const int V = p.V, turns = (V + 8191) / 8192;
+    constexpr int WAVES = THREADS / 64, TURN = 8 * THREADS, BINS = 2 * THREADS, LIST = THREADS, ROLL = HELD * THREADS;
+    __shared__ Shared<THREADS> sh;
+    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), r = blockIdx.x, b = blockIdx.y;
+    const int V = p.V, turns = (V + TURN - 1) / TURN;
     const void *row = (const char *)p.x + ((int64_t)b * p.x_batch + (int64_t)r * p.x_row) * (F32 ? 4 : 2);
-    Eight<F32> kept_row[NIT > 0 ? NIT : 1];
-    if constexpr (NIT > 0) {
-#pragma unroll
-        for (int t = 0; t < NIT; ++t) kept_row[t].load(row, (t * THREADS + tid) * 8, V);
-    }
-    // f(turn, first index, eight logits); from memory four at a time
+    // f(turn, first index, eight logits), those from memory requested some turns ahead.  (In a loop, as every pass has its own code: of a
+    // row in registers with the code of every token in it, 7 passes over 32 a thread, fetching the code took longer than all else.)
+    constexpr int AHEAD = 2;
     auto each = [&](auto f) __attribute__((always_inline)) {
-        if constexpr (NIT > 0) {
+        Eight<F32> x[AHEAD];
 #pragma unroll
-            for (int t = 0; t < NIT; ++t) {
-                kept_row[t].anew();
-                if (t < turns) f(t, (t * THREADS + tid) * 8, kept_row[t]);
-                __builtin_amdgcn_sched_barrier(0);
-            }
-        } else {
-            for (int t0 = 0; t0 < turns; t0 += 4) {
-                Eight<F32> x[4];
+        for (int k = 0; k < AHEAD; ++k) x[k].load(row, (k * THREADS + tid) * 8, V);
+#pragma unroll 1
+        for (int t = 0; t < turns; ++t) {
+            const Eight<F32> now = x[0];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) x[k].load(row, ((t0 + k) * THREADS + tid) * 8, V);
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    if (t0 + k < turns) f(t0 + k, ((t0 + k) * THREADS + tid) * 8, x[k]);
-            }
+            for (int k = 0; k + 1 < AHEAD; ++k) x[k] = x[k + 1];
+            if (t + AHEAD < turns) x[AHEAD - 1].load(row, ((t + AHEAD) * THREADS + tid) * 8, V);
+            f(t, (t * THREADS + tid) * 8, now);
         }
     };
     // over the workgroup: sums, maxima; all threads get them
@@ -191,18 +183,24 @@ __global__ __launch_bounds__(THREADS) void sample_rows_kernel(const SampleParams
         __syncthreads();
         if (lane == 0) sh.wave[wave] = v;
         __syncthreads();
-        u64 s = 0;
-        for (int k = 0; k < WAVES; ++k) s += sh.wave[k];
-        return s;
+        return wave_sum(lane < WAVES ? sh.wave[lane] : 0);
     };
     auto block_max = [&](u64 v) {
         v = wave_largest(v);
         __syncthreads();
         if (lane == 0) sh.wave[wave] = v;
         __syncthreads();
-        u64 s = 0;
-        for (int k = 0; k < WAVES; ++k) s = sh.wave[k] > s ? sh.wave[k] : s;
-        return s;
+        return wave_largest(lane < WAVES ? sh.wave[lane] : 0);
+    };
+    // sum of those before this thread, and of all
+    auto block_scan = [&](u64 v, u64 &all) {
+        const u64 in = wave_scan(v);
+        __syncthreads();
+        if (lane == 63) sh.wave[wave] = in;
+        __syncthreads();
+        const u64 waves = wave_scan(lane < WAVES ? sh.wave[lane] : 0);
+        all = lane_of(waves, WAVES - 1);
+        return in - v + (wave ? lane_of(waves, wave - 1) : 0);
     };
     float *probs = p.probs ? p.probs + (int64_t)b * p.p_batch + (int64_t)r * V : nullptr;
     int32_t *tokens = p.tokens ? p.tokens + (int64_t)b * p.t_batch + (int64_t)r * p.n_draw : nullptr;
@@ -270,26 +268,31 @@ __global__ __launch_bounds__(THREADS) void sample_rows_kernel(const SampleParams
         if (tid == 0) sh.listed = 0;
         __syncthreads();
     };
-    // Where the sum over the 2048 places reaches goal(sum of all): sh.bin, and sh.above up to there; above: what is before the first of them.
+    // Where the sum over the places reaches goal(sum of all): sh.bin, and sh.above up to there; above: what is before the first of them.
     u64 target = 0;
     auto choose = [&](u64 above, auto goal) {
         __syncthreads();
-        const u64 h0 = sh.hist[2 * tid], h1 = sh.hist[2 * tid + 1], in = wave_scan(h0 + h1);
-        if (lane == 63) sh.wave2[wave] = in;
-        __syncthreads();
-        u64 before = above + in - (h0 + h1), all = above;
-        for (int k = 0; k < WAVES; ++k) {
-            all += sh.wave2[k];
-            if (k < wave) before += sh.wave2[k];
-        }
-        target = goal(all);
+        const u64 h0 = sh.hist[2 * tid], h1 = sh.hist[2 * tid + 1];
+        u64 all;
+        const u64 before = above + block_scan(h0 + h1, all);
+        target = goal(above + all);
         if (before < target && before + h0 >= target) { sh.bin = 2 * tid; sh.above = before; }
         if (before + h0 < target && before + h0 + h1 >= target) { sh.bin = 2 * tid + 1; sh.above = before + h0; }
         __syncthreads();
     };
-    auto append = [&](u64 place) __attribute__((always_inline)) {
-        const int n = atomicAdd(&sh.listed, 1);
-        if (n < LIST) sh.list[n].place = place;
+    // The wanted ones of eight tokens behind the list: one place asked for per wavefront.
+    auto append = [&](const Eight<F32> &x, int i, unsigned wanted) __attribute__((always_inline)) {
+        const int here = __builtin_popcount(wanted), in = ::wave_scan(here), all = ::wave_last(in);
+        if (all == 0) return;
+        int n = 0;
+        if (lane == 63) n = atomicAdd(&sh.listed, all);
+        n = ::wave_last(n) + in - here;
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (wanted >> k & 1) {
+                if (n < LIST) sh.list[n].place = place_of(x[k], i + k);
+                ++n;
+            }
     };
     // Every thread has one of the n listed tokens: its place (0: none), its measure, and that of all tokens before it in the order.
     u64 mine = 0, own = 0, before_me = 0;
@@ -316,7 +319,8 @@ __global__ __launch_bounds__(THREADS) void sample_rows_kernel(const SampleParams
     };
     // The place at which the sum of measure(logit) over the tokens from the first on reaches goal(sum of all) >= 1 becomes the cut; returns
     // the sum up to and with it.
-    auto find = [&](auto measure, auto goal) -> u64 {
+    auto find = [&](bool by_weight, auto goal) -> u64 {
+        auto measure = [&](float x) __attribute__((always_inline)) { return by_weight ? weight(x) : (u64)1; };
         const float range = 31.9f * T, scale = range < INFINITY ? (BINS - 0.5f) / range : 0.f;      // (weights are zero beyond it)
         auto bin_of = [&](float x) { return scale < INFINITY ? (int)fminf((mx - x) * scale, (float)(BINS - 1)) : 0; };
         clear();
@@ -332,9 +336,10 @@ __global__ __launch_bounds__(THREADS) void sample_rows_kernel(const SampleParams
         const int bin = sh.bin;
         u64 above = sh.above, lo = 0, hi = ~0ull;
         each_kept([&](int, int i, const Eight<F32> &x) __attribute__((always_inline)) {
+            unsigned wanted = 0;
 #pragma unroll
-            for (int k = 0; k < 8; ++k)
-                if (bin_of(x[k]) == bin && kept(x[k], i + k)) append(place_of(x[k], i + k));
+            for (int k = 0; k < 8; ++k) wanted |= bin_of(x[k]) == bin && kept(x[k], i + k) ? 1u << k : 0;
+            append(x, i, wanted);
         }, cut_x);
         __syncthreads();
         bool parted = false;
@@ -375,11 +380,13 @@ __global__ __launch_bounds__(THREADS) void sample_rows_kernel(const SampleParams
                 hi = end;
                 lo = begin > lo && begin <= end ? begin : lo;
                 each([&](int, int i, const Eight<F32> &x) __attribute__((always_inline)) {
+                    unsigned wanted = 0;
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {
                         const u64 at = place_of(x[k], i + k);
-                        if (at >= lo && at <= hi) append(at);
+                        wanted |= at >= lo && at <= hi ? 1u << k : 0;
                     }
+                    append(x, i, wanted);
                 });
                 __syncthreads();
             }
@@ -434,9 +441,10 @@ __global__ __launch_bounds__(THREADS) void sample_rows_kernel(const SampleParams
             auto wanted = [&](float x) { return x >= cut_x && (x >= low ? bin_of(x) <= bin : bin == BINS); };
             each([&](int, int i, const Eight<F32> &x) __attribute__((always_inline)) {
                 if (__builtin_amdgcn_ballot_w64(wanted(max8(x))) == 0) return;
+                unsigned these = 0;
 #pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    if (wanted(x[k])) append(place_of(x[k], i + k));
+                for (int k = 0; k < 8; ++k) these |= wanted(x[k]) ? 1u << k : 0;
+                append(x, i, these);
             });
             __syncthreads();
             const int n = sh.listed;
@@ -444,11 +452,9 @@ __global__ __launch_bounds__(THREADS) void sample_rows_kernel(const SampleParams
             if (n <= LIST) settle(n, top_k);
         }
         if (!exact) {
-            if (some) find([](float) { return (u64)1; }, [&](u64 all) { return all < (u64)top_k ? all : (u64)top_k; });
-            if (top_p < 1.f) {
-                sum = find(weight, share);
-                exact = !(min_p > 0.f);
-            }
+            for (int by_weight = !some; by_weight <= (top_p < 1.f); ++by_weight)      // (one after the other: one piece of code)
+                sum = find(by_weight, [&](u64 all) { return by_weight ? share(all) : all < (u64)top_k ? all : (u64)top_k; });
+            exact = top_p < 1.f && !(min_p > 0.f);
             by_min_p = min_p > 0.f;
         }
     }
@@ -483,7 +489,10 @@ __global__ __launch_bounds__(THREADS) void sample_rows_kernel(const SampleParams
     // Weights in fp32: the difference and its product with log2(e) / T in two parts each, the second of which multiplies the exponential.
     // (By way of binary64 its conversions cost most: 110 cycles of a SIMD per 64 tokens, so 60.  That way is for what fp32 does not hold.)
     const float c_hi = (float)c, c_lo = (float)(c - (double)c_hi);
-    const bool beyond = !(c < 1e30) || mx > 1e37f;
+    const double zero_x = mxd - 151.0 / c;                                 // (powers are zero from there down; masks are as low as -3.4e38)
+    const bool beyond = !(c < 1e30) || mx > 1e37f || !(fabs(mxd) * c < 1e30) || !(zero_x > -1e38);
+    float floor_x = (float)zero_x;
+    if ((double)floor_x > zero_x) floor_x = of_ordered(ordered(floor_x) - 1);
     auto powers = [&](const Eight<F32> &x, float (&e)[8]) __attribute__((always_inline)) {
         if (__builtin_expect(beyond, 0)) {
 #pragma unroll
@@ -496,12 +505,14 @@ __global__ __launch_bounds__(THREADS) void sample_rows_kernel(const SampleParams
         }
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-            const float d = x[k] - mx, back = d + mx, lost = (x[k] - back) + ((back - d) - mx);      // x - mx = d + lost
+            const float v = fmaxf(x[k], floor_x), d = v - mx, back = d + mx, lost = (v - back) + ((back - d) - mx);      // v - mx = d + lost
             const float y = d * c_hi, rest = fmaf(lost, c_hi, fmaf(d, c_lo, fmaf(d, c_hi, -y))), w = __builtin_amdgcn_exp2f(y);
-            e[k] = y > -150.f ? fmaf(w * rest, 0.69314718f, w) : 0.f;      // (masks are as low as -3.4e38)
+            e[k] = fmaf(w * rest, 0.69314718f, w);
             if (k % 4 == 3) __builtin_amdgcn_sched_barrier(0);
         }
     };
+    // Nothing is cut off (and what is minus infinity has a power of zero by itself).
+    const bool whole = all_equal_kept && !by_min_p && !beyond && cut_x == -3.402823466e38f;
     float inv = 0.f;
     if (exact || p.n_draw) {
         if (!exact) sum = 0;
@@ -510,8 +521,9 @@ __global__ __launch_bounds__(THREADS) void sample_rows_kernel(const SampleParams
         each([&](int, int i, const Eight<F32> &x) __attribute__((always_inline)) {
             float e[8];
             powers(x, e);
+            if (!whole)
 #pragma unroll
-            for (int k = 0; k < 8; ++k) e[k] = kept(x[k], i + k) ? e[k] : 0.f;
+                for (int k = 0; k < 8; ++k) e[k] = kept(x[k], i + k) ? e[k] : 0.f;
             part += (double)(((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7])));
         });
         // (in the order of the lanes and wavefronts: the same every time)
@@ -520,8 +532,9 @@ __global__ __launch_bounds__(THREADS) void sample_rows_kernel(const SampleParams
         __syncthreads();
         if (lane == 0) sh.wave[wave] = __builtin_bit_cast(u64, part);
         __syncthreads();
-        double all = 0.0;
-        for (int k = 0; k < WAVES; ++k) all += __builtin_bit_cast(double, sh.wave[k]);
+        double all = lane < WAVES ? __builtin_bit_cast(double, sh.wave[lane]) : 0.0;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) all += __shfl_xor(all, o);
         inv = (float)(1.0 / all);
     }
 
@@ -539,16 +552,7 @@ __global__ __launch_bounds__(THREADS) void sample_rows_kernel(const SampleParams
             roll_w[k] = alive >> k & 1 ? weight(roll_x[k]) : 0;
             here += roll_w[k];
         }
-        const u64 in = wave_scan(here);
-        __syncthreads();
-        if (lane == 63) sh.wave[wave] = in;
-        __syncthreads();
-        before_roll = in - here;
-        sum = 0;
-        for (int k = 0; k < WAVES; ++k) {
-            if (k < wave) before_roll += sh.wave[k];
-            sum += sh.wave[k];
-        }
+        before_roll = block_scan(here, sum);
     };
     if (p.n_draw) {
         const int segments = turns * WAVES;
@@ -607,7 +611,11 @@ __global__ __launch_bounds__(THREADS) void sample_rows_kernel(const SampleParams
     if (probs) {
         each([&](int, int i, const Eight<F32> &x) __attribute__((always_inline)) {
             float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-            if (__builtin_amdgcn_ballot_w64(max8(x) >= cut_x) != 0) {      // (the other wavefronts have zeros to write)
+            if (whole) {
+                powers(x, y);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) y[k] *= inv;
+            } else if (__builtin_amdgcn_ballot_w64(max8(x) >= cut_x) != 0) {      // (the other wavefronts have zeros to write)
                 powers(x, y);
 #pragma unroll
                 for (int k = 0; k < 8; ++k) y[k] = kept(x[k], i + k) ? y[k] * inv : 0.f;
@@ -794,8 +802,11 @@ extern "C" int mcsd_sample_rows(mcsd_dtype_t dtype, int32_t B, int32_t W, int32_
     p.probs = probs; p.p_batch = probs_batch_stride;
     p.n_draw = n_draw; p.distinct = sampling == MCSD_WITHOUT_REPLACEMENT; p.u = u; p.tokens = n_draw ? tokens : nullptr; p.t_batch = tokens_batch_stride;
     const bool f32 = dtype == MCSD_F32;
-    auto kernel = f32 ? (V <= 8192 ? sample_rows_kernel<true, 1> : V <= 32768 ? sample_rows_kernel<true, 4> : sample_rows_kernel<true, 0>)
-                      : (V <= 8192 ? sample_rows_kernel<false, 1> : V <= 32768 ? sample_rows_kernel<false, 4> : V <= 65536 ? sample_rows_kernel<false, 8> : sample_rows_kernel<false, 0>);
-    hipLaunchKernelGGL(kernel, dim3((unsigned)W, B), dim3(THREADS), 0, (hipStream_t)hip_stream, p);
+    // Fewer rows than compute units: all of a compute unit's wavefronts that fit, on one row (512 threads: 24 / 75 / 203 us where 1024 take
+    // 22 / 50 / 157); more: two workgroups to a compute unit, one's meetings under the other's passes (188 us where 1024 threads take 255).
+    const bool wide = W * (int64_t)B <= mcsd_compute_units();
+    auto kernel = wide ? (f32 ? sample_rows_kernel<true, 1024> : sample_rows_kernel<false, 1024>)
+                       : (f32 ? sample_rows_kernel<true, 512> : sample_rows_kernel<false, 512>);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)W, B), dim3(wide ? 1024 : 512), 0, (hipStream_t)hip_stream, p);
     return mcsd_hip_status(hipGetLastError());
 }

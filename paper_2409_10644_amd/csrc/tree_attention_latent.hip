@@ -647,22 +647,6 @@ struct LatentPlan {
 
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
-int compute_units()
-{
-    static std::atomic<int> cus_of_device[64];
-    int dev = 0;
-    if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) {
-        (void)hipGetLastError();
-        return 256;                  // no device to ask: the whole chip
-    }
-    int v = cus_of_device[dev].load(std::memory_order_relaxed);
-    if (v == 0) {
-        if (hipDeviceGetAttribute(&v, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || v < 1) v = 256;
-        cus_of_device[dev].store(v, std::memory_order_relaxed);
-    }
-    return v;
-}
-
 // False where the work has more tiles than the kernel's numbers hold.
 bool make_plan(int B, int H, int dl, int n_rows, int n, int max_prefix, LatentPlan &pl)
 {
@@ -670,7 +654,7 @@ bool make_plan(int B, int H, int dl, int n_rows, int n, int max_prefix, LatentPl
     const int64_t tiles = (n + KEYS - 1) / KEYS + ((int64_t)max_prefix + KEYS - 1) / KEYS;
     if (rows > 0x3fffffff || pairs > 0x3fffffff || pairs * tiles > 0x3fffffff) return false;
     const int64_t pieces = pairs * ((tiles + MIN_TILES - 1) / MIN_TILES);
-    const int cus = compute_units();
+    const int cus = mcsd_compute_units();
     pl.chunks = (int)chunks;
     pl.workgroups = (int)(pieces < cus ? pieces : cus);
     pl.slot_rows = rows < ROWS ? (int)rows : ROWS;

@@ -57,6 +57,31 @@ def run(binding, x, settings, us=None, distinct=False, probs=True, skew=0, pad=0
 ALL = [(1.0, 0, 1.0, 0.0), (0.7, 50, 0.9, 0.02), (1.3, 0, 0.95, 0.0), (0.3, 7, 1.0, 0.0), (0.0, 5, 0.5, 0.5), (2.0, 0, 1.0, 0.2), (0.9, 1, 1.0, 0.0), (1.0, 10 ** 9, 0.3, 0.001)]
 
 
+@pytest.mark.parametrize("dtype", CODE)
+@pytest.mark.parametrize("V", [1, 9, 511, 4095, 4096, 4097, 33003, 262144])
+@pytest.mark.parametrize("distinct", [None, False, True])
+def test_more_rows_than_compute_units(binding, dtype, V, distinct):
+    """Rows of a large batch go two to a compute unit; every row is what it is in a small one."""
+    gen = torch.Generator("cuda").manual_seed(V + 1)
+    B, W, n = len(ALL), 2, 0 if distinct is None else 5
+    x, us = _logits(gen, B, W, V, dtype), torch.rand(B, W, n, generator=gen, device="cuda") if n else None
+    p, tokens = run(binding, x, ALL, us, distinct)
+    copies = torch.cuda.get_device_properties(0).multi_processor_count // (B * W) + 1
+    arrays, _ = _settings(ALL)
+    many = torch.empty(B * copies * W * V, device="cuda")
+    many_tokens = torch.empty(B, copies * W * n, dtype=torch.int32, device="cuda") if n else None
+    binding.sample_rows(CODE[dtype], B, copies * W, V, x.repeat(1, copies, 1), copies * W * V, V, binding.make_sampler(*arrays), many, copies * W * V,
+                        binding.MCSD_WITHOUT_REPLACEMENT if distinct else binding.MCSD_WITH_REPLACEMENT, n, us.repeat(1, copies, 1) if n else None, many_tokens, copies * W * n)
+    torch.cuda.synchronize()
+    many = many.view(B, copies, W * V)
+    # the copies alike, and off from the small call's by a step of 1 / sum (2^-23) and half a step of each product
+    assert torch.equal(many, many[:, :1].expand_as(many))
+    p = p.view(B, W * V)
+    assert bool(((many[:, 0] - p).abs() <= 4 * 2.0 ** -24 * p + 2.0 ** -149).all()), (many[:, 0] - p).abs().max()
+    if n:
+        assert torch.equal(many_tokens.view(B, copies, W * n), tokens[:, :W * n].reshape(B, 1, W * n).expand(B, copies, W * n))
+
+
 def _logits(gen, B, W, V, dtype, spread=3.0):
     x = spread * torch.randn(B, W, V, generator=gen, device="cuda")
     if V > 20:
