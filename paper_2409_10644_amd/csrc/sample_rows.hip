@@ -12,10 +12,10 @@
 // so a border falls where 64 bits have it.  Probabilities are computed in fp32 pairs, or of a binary64 exponent.
 //
 // What bounds it, at 32000 logits a row: few rows, the passes and meetings of one workgroup one after the other (45 rows of bf16, top-k 50
-// with top-p and min-p: 22 us; 64 rows of fp32 with top-p and four distinct draws: 50 us; 32 rows of 131077, mixed: 157 us, most of it
-// the binary64 weights of the rows with a top-p alone); many rows, the exponentials, made once for the sum and once for the row
-// (2816 rows of bf16: 187 us for 541 MB, 2.9 TB/s; kept between the two they would need the LDS that the second workgroup has).
-// Rows in LDS between the passes took 24 / 70 / - / 276 us for these four, two rows requested ahead more 22.6 / 57 / 166 / 187.
+// with top-p and min-p: 21 us; 64 rows of fp32 with top-p and four distinct draws: 46 us; 32 rows of 131077, mixed: 135 us, the vector
+// instructions of the rows with a top-p alone, 7 in 10 cycles); many rows, the exponentials, made once for the sum and once for the row
+// (2816 rows of bf16: 185 us for 541 MB, 2.9 TB/s; kept between the two they would need the LDS that the second workgroup has).
+// Rows in LDS between the passes took 2 to 20 us longer, and so did requests two more turns ahead.
 #include <math.h>
 
 #include "mcsd_internal.h"
@@ -77,7 +77,8 @@ __device__ __forceinline__ int index_of(u64 place) { return 0x3ffff - (int)(plac
 __device__ __forceinline__ u64 weight_of(double y)
 {
     y = fmax(y, -60.0);                                                    // (zero, without a branch)
-    const double n = rint(y), f = y - n;
+    const double shifted = y + 0x1.8p52, f = y - (shifted - 0x1.8p52);      // (the integer next to y: without the conversions, a quarter as fast)
+    const int n = (int)__builtin_bit_cast(u64, shifted);
     double p = 0x1.e6063f7217bc6p-28;
     p = fma(p, f, 0x1.b675bca4eeebbp-24);
     p = fma(p, f, 0x1.62bfd47773353p-20);
@@ -89,8 +90,8 @@ __device__ __forceinline__ u64 weight_of(double y)
     p = fma(p, f, 0x1.ebfbdff82c598p-3);
     p = fma(p, f, 0x1.62e42fefa3a19p-1);
     p = fma(p, f, 1.0);
-    // (2^52 added: the sum's last place is 1)
-    const double s = ldexp(p, (int)n + ONE) + 0x1p52;
+    // (times 2^(n + 45), and 2^52 added: the sum's last place is 1)
+    const double s = fma(p, __builtin_bit_cast(double, (u64)(unsigned)(n + ONE + 1023) << 52), 0x1p52);
     return __builtin_bit_cast(u64, s) & 0xfffffffffffffull;
 }
 
@@ -237,19 +238,16 @@ __global__ __launch_bounds__(THREADS, 4) void sample_rows_kernel(const SamplePar
         return;
     }
 
-    // ---- the cut: a token is kept if its place is not below it, and its exponent not below min_y
+    // ---- the cut: a token is kept if its logit is above it, or at it and its index not behind
     const double c = T > 0.f ? 1.4426950408889634074 / (double)T : 0.0, mxd = (double)mx;
     const double min_y = min_p > 0.f ? fmin(log2((double)min_p), 0.0) : -INFINITY;
     double top = mxd;                                                      // what weights are relative to
-    float cut_x = -3.402823466e38f;                                        // the cut's logit: of everything but minus infinity
-    int cut_i = 0;                                                         // and index; tokens of that logit are kept up to it, unless all are
-    bool all_equal_kept = true, by_min_p = false;
+    constexpr float LOWEST = -3.402823466e38f;
+    float cut_x = LOWEST;                                                  // of everything but minus infinity
+    int cut_i = V;
     auto exponent = [&](float x) { return ((double)x - mxd) * c; };
     auto weight = [&](float x) { return weight_of(((double)x - top) * c); };
-    auto kept = [&](float x, int i) __attribute__((always_inline)) {
-        const bool in = all_equal_kept ? x >= cut_x : x > cut_x || (x == cut_x && i <= cut_i);
-        return by_min_p ? in && exponent(x) >= min_y : in;
-    };
+    auto kept = [&](float x, int i) __attribute__((always_inline)) { return x > cut_x || (x == cut_x && i <= cut_i); };
     // each, but for wavefronts without a token from this logit on
     auto max8 = [](const Eight<F32> &x) { return fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7]))); };
     auto each_kept = [&](auto f, float from) __attribute__((always_inline)) {
@@ -259,8 +257,7 @@ __global__ __launch_bounds__(THREADS, 4) void sample_rows_kernel(const SamplePar
     };
     auto set_cut = [&](u64 place, bool whole) {
         cut_x = of_ordered((unsigned)(place >> 18));
-        cut_i = index_of(place);
-        all_equal_kept = whole;
+        cut_i = whole ? V : index_of(place);
     };
     auto clear = [&]() {
         sh.hist[tid] = 0;
@@ -282,8 +279,8 @@ __global__ __launch_bounds__(THREADS, 4) void sample_rows_kernel(const SamplePar
     };
     // The wanted ones of eight tokens behind the list: one place asked for per wavefront.
     auto append = [&](const Eight<F32> &x, int i, unsigned wanted) __attribute__((always_inline)) {
+        if (__builtin_amdgcn_ballot_w64(wanted != 0) == 0) return;
         const int here = __builtin_popcount(wanted), in = ::wave_scan(here), all = ::wave_last(in);
-        if (all == 0) return;
         int n = 0;
         if (lane == 63) n = atomicAdd(&sh.listed, all);
         n = ::wave_last(n) + in - here;
@@ -454,8 +451,20 @@ __global__ __launch_bounds__(THREADS, 4) void sample_rows_kernel(const SamplePar
         if (!exact) {
             for (int by_weight = !some; by_weight <= (top_p < 1.f); ++by_weight)      // (one after the other: one piece of code)
                 sum = find(by_weight, [&](u64 all) { return by_weight ? share(all) : all < (u64)top_k ? all : (u64)top_k; });
-            exact = top_p < 1.f && !(min_p > 0.f);
-            by_min_p = min_p > 0.f;
+            exact = top_p < 1.f;
+            if (min_p > 0.f) {                                             // the lowest logit that it keeps, between minus infinity and mx
+                unsigned out = ordered(-INFINITY), in = ordered(mx);
+                while (in - out > 1) {
+                    const unsigned mid = out + (in - out) / 2;
+                    if (exponent(of_ordered(mid)) >= min_y) in = mid;
+                    else out = mid;
+                }
+                if (of_ordered(in) > cut_x) {
+                    cut_x = of_ordered(in);
+                    cut_i = V;
+                    exact = false;
+                }
+            }
         }
     }
 
@@ -512,7 +521,7 @@ __global__ __launch_bounds__(THREADS, 4) void sample_rows_kernel(const SamplePar
         }
     };
     // Nothing is cut off (and what is minus infinity has a power of zero by itself).
-    const bool whole = all_equal_kept && !by_min_p && !beyond && cut_x == -3.402823466e38f;
+    const bool whole = cut_x == LOWEST && cut_i == V && !beyond;
     float inv = 0.f;
     if (exact || p.n_draw) {
         if (!exact) sum = 0;
@@ -802,8 +811,8 @@ extern "C" int mcsd_sample_rows(mcsd_dtype_t dtype, int32_t B, int32_t W, int32_
     p.probs = probs; p.p_batch = probs_batch_stride;
     p.n_draw = n_draw; p.distinct = sampling == MCSD_WITHOUT_REPLACEMENT; p.u = u; p.tokens = n_draw ? tokens : nullptr; p.t_batch = tokens_batch_stride;
     const bool f32 = dtype == MCSD_F32;
-    // Fewer rows than compute units: all of a compute unit's wavefronts that fit, on one row (512 threads: 24 / 75 / 203 us where 1024 take
-    // 22 / 50 / 157); more: two workgroups to a compute unit, one's meetings under the other's passes (188 us where 1024 threads take 255).
+    // Fewer rows than compute units: all of a compute unit's wavefronts that fit, on one row (512 threads took 25 / 75 / 204 us for the first
+    // three above where 1024 took 22 / 50 / 157); more: two workgroups to a compute unit, one's meetings under the other's passes (188 us where 1024 threads took 255).
     const bool wide = W * (int64_t)B <= mcsd_compute_units();
     auto kernel = wide ? (f32 ? sample_rows_kernel<true, 1024> : sample_rows_kernel<false, 1024>)
                        : (f32 ? sample_rows_kernel<true, 512> : sample_rows_kernel<false, 512>);
