@@ -523,11 +523,13 @@ int mcsd_prompt_qk_norm_rope(mcsd_dtype_t dtype, int32_t B, int32_t H_q, int32_t
  *                 and the first 64 KiB + 256 bytes stay as they are, so a workspace of the other attention calls serves as well.  The
  *                 size for a call serves calls of the same B, H and sizes with fewer nodes, rows or prefix keys.  Calls that share a
  *                 workspace must be ordered on one stream.
+ * NaN and infinities of a tree node's row make the output rows that see it NaN, and no others; those of a prefix row reach all rows of
+ * its sequence.
  * Scores, soft-max statistics and sums are fp32; weights are rounded to bf16 for the product with the values; partial results of split
  * keys are exchanged in fp32 and folded in a fixed order.  One launch, a second one where keys may be split.
  * Accepted rows join the cache through mcsd_commit_path with H = 1, d = d_latent + d_rope, head_stride 0 and the same arrays as keys
  * and as values.
- * Errors: MCSD_EUNSUPPORTED for other sizes, too many nodes, or more than 2^30 tiles of 64 rows and 64 keys; MCSD_EINVAL also for a mask
+ * Errors: MCSD_EUNSUPPORTED for other sizes, too many nodes, or 2^30 tiles of 64 rows and 32 keys or more; MCSD_EINVAL also for a mask
  * of another device than the current one.
  * ------------------------------------------------------------------------------------------------- */
 size_t mcsd_tree_attention_latent_workspace(int32_t B, int32_t H, int32_t d_latent, int32_t d_rope, int32_t n_nodes,

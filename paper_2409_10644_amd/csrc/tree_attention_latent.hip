@@ -54,6 +54,7 @@ constexpr float SLACK = 16.f;        // log2 of what a score may exceed the runn
 constexpr int ROWS = 64, KEYS = 32;  // query rows of a chunk, keys of a tile
 constexpr int MIN_TILES = 4, CROSS = 12;
 constexpr int THREADS = 512;
+constexpr int GROWN = 1, WRONG = 2;  // of a tile: scores beyond a reference; scores of tree nodes, seen or not, that are not finite
 
 __device__ __align__(64) const unsigned char no_row[128] = {};
 
@@ -151,6 +152,24 @@ __device__ __forceinline__ void multiply(int on, f32x4_t (&o)[4][8], int a, int 
                    [f] "=&v"(f), [t0] "=&v"(t0), [t1] "=&v"(t1), [t2] "=&v"(t2), [t3] "=&v"(t3)
                  : [a] "v"(a), [own] "v"(own), [on] "s"(on)
                  : "memory", "scc");
+}
+
+// Values of a tree tile that are not finite become zeros, in the panels that one wavefront of O^T reads (the scores are made by then).
+// Rows that do not see such a node have a weight of zero for it, and the product with its values would be NaN; a row that sees it is NaN by
+// its score.
+__device__ __forceinline__ void clear_wrong(unsigned char *panels, int lane, int bytes)
+{
+#pragma unroll 1
+    for (int k = lane * 16; k < bytes; k += 1024) {
+        u32x4_t v = *(const u32x4_t *)(panels + k);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if ((v[i] & 0x7f80u) == 0x7f80u) v[i] &= 0xffff0000u;
+            if ((v[i] & 0x7f800000u) == 0x7f800000u) v[i] &= 0xffffu;
+        }
+        *(u32x4_t *)(panels + k) = v;
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 }
 
 // A tile in LDS: panels of 64 channels, 128 bytes a row (the last panel has the d_rope channels).  The 16-byte chunk c of row r stands at
@@ -397,7 +416,7 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(2, 2)))
                     if (ks + AHEAD < C::KS) kf[ks % AHEAD] = key_of(ks + AHEAD);
                 }
                 __builtin_amdgcn_sched_barrier(0);
-                if (t > 0 && __builtin_expect(uniform((int)(flags[0] | flags[1] | flags[2] | flags[3])) != 0, 0)) outgrown(t - 1);
+                if (t > 0 && __builtin_expect((uniform((int)(flags[0] | flags[1] | flags[2] | flags[3])) & GROWN) != 0, 0)) outgrown(t - 1);
                 settle();
 #pragma unroll
                 for (int rg = 0; rg < 2; ++rg) {
@@ -407,10 +426,18 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(2, 2)))
                 }
                 const bool tree = at < tree_tiles;
                 const int here = tree ? KEYS : len - (at - tree_tiles) * KEYS;
+                bool wrong = false;
                 if (tree || here < KEYS) {
                     unsigned bits;
                     if (tree) {
                         bits = seen >> (8 * at);
+#pragma unroll
+                        for (int rg = 0; rg < 2; ++rg)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                s[rg][i] += s[rg][i] - s[rg][i];           // (infinities as well are NaN)
+                                wrong |= s[rg][i] != s[rg][i];
+                            }
                     } else {
                         const int mine = min(max(here - 16 * kg - 4 * grp, 0), 4);
                         bits = ((1u << mine) - 1) * 0x11u;
@@ -424,14 +451,14 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(2, 2)))
                 bool grow = false;
 #pragma unroll
                 for (int rg = 0; rg < 2; ++rg) grow |= max4(s[rg]) * p.c > ref[rg] + SLACK;
-                const bool wave_grows = __builtin_amdgcn_ballot_w64(grow) != 0;
-                if (lane == 0) *(int *)(lds + C::FLAG_AT + (t & 1) * 16 + 4 * wave) = wave_grows;
+                const int flag = (__builtin_amdgcn_ballot_w64(grow) != 0 ? GROWN : 0) | (__builtin_amdgcn_ballot_w64(wrong) != 0 ? WRONG : 0);
+                if (lane == 0) *(int *)(lds + C::FLAG_AT + (t & 1) * 16 + 4 * wave) = flag;
                 __builtin_amdgcn_s_setprio(0);
                 meet();
             }
             {
                 const u32x4_t flags = flagged(count - 1);
-                if (__builtin_expect(uniform((int)(flags[0] | flags[1] | flags[2] | flags[3])) != 0, 0)) outgrown(count - 1);
+                if (__builtin_expect((uniform((int)(flags[0] | flags[1] | flags[2] | flags[3])) & GROWN) != 0, 0)) outgrown(count - 1);
                 l[0] += sum[0];
                 l[1] += sum[1];
             }
@@ -499,8 +526,13 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(2, 2)))
                 for (int cb = 0; cb < AHEAD; ++cb) vf[cb] = value_of(cb);
                 __builtin_amdgcn_sched_barrier(0);
                 asm volatile("" : "+v"(pf[0]), "+v"(pf[1]), "+v"(pf[2]), "+v"(pf[3]));       // (one wait for weights and flags)
-                const int on = uniform((int)(flags[0] | flags[1] | flags[2] | flags[3]));      // whether a reference was outgrown by that tile
-                if (__builtin_expect(on != 0, 0)) {
+                const int flag = uniform((int)(flags[0] | flags[1] | flags[2] | flags[3])), on = flag & GROWN;
+                if (__builtin_expect((flag & WRONG) != 0, 0)) {
+                    clear_wrong(lds + ((t - 1) & 3) * C::TILE + part * (DL / 4) * (2 * KEYS), lane, DL / 4 * (2 * KEYS));
+#pragma unroll
+                    for (int cb = 0; cb < AHEAD; ++cb) vf[cb] = value_of(cb);
+                }
+                if (__builtin_expect(on != 0, 0)) {                        // a reference was outgrown by that tile
                     meet();
                     meet();
 #pragma unroll
