@@ -592,7 +592,8 @@ int mcsd_store_latent(mcsd_dtype_t dtype, int32_t B, int32_t d_latent, int32_t d
  * u       : DEVICE fp32 [B][W*n_draw] in [0,1)  (kept within it);   0 <= n_draw <= MCSD_MAX_BRANCH
  * tokens  : DEVICE int32; draw d of row r of sequence b at b*tokens_batch_stride + r*n_draw + d: with the rows of a level's contexts in
  *           node order, and tokens pointing at the next level's first node, the children of each context
- * Limits: V <= MCSD_MAX_VOCAB, W < 2^22.  Rows that are written must not share places (MCSD_EINVAL).  One launch, no workspace.
+ * Limits: V <= MCSD_MAX_VOCAB, W < 2^22.  Rows that are written must not share places, nor probs begin at logits (MCSD_EINVAL);
+ * outputs must not overlap inputs.  One launch, no workspace.
  * ------------------------------------------------------------------------------------------------- */
 typedef struct mcsd_sampler {
     const float *temperature;

@@ -805,6 +805,7 @@ extern "C" int mcsd_sample_rows(mcsd_dtype_t dtype, int32_t B, int32_t W, int32_
     const uintptr_t element = dtype == MCSD_F32 ? 3 : 1;
     if (((uintptr_t)logits & element) || (((uintptr_t)probs | (uintptr_t)u | (uintptr_t)tokens) & 3)) return MCSD_EINVAL;
     if (V > MCSD_MAX_VOCAB || n_draw > MAX_DRAW || W > MCSD_MAX_GRID_1024) return MCSD_EUNSUPPORTED;
+    if (probs && (const void *)probs == logits) return MCSD_EINVAL;        // (logits are read again behind the first probabilities)
 
     SampleParams p = {};
     p.x = logits; p.x_batch = batch_stride; p.x_row = row_stride; p.W = W; p.V = V; p.s = *sampler;
