@@ -99,7 +99,8 @@ __device__ __forceinline__ float row_sum(float v)
 }
 
 // Matrix products with the accumulator in its place (the builtin's result may stand elsewhere, and across a loop's branches it then
-// does: twice the registers).  The wait states that vector instructions need behind the results are the caller's: settle().
+// does: twice the registers).  The wait states that vector instructions need behind the results are the caller's, settle(), and so are the
+// two between a vector instruction and a product that reads what it wrote.
 __device__ __forceinline__ void mfma(f32x4_t &c, const bf16x8_t &a, const bf16x8_t &b) { asm("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+v"(c) : "v"(a), "v"(b)); }
 __device__ __forceinline__ void settle() { asm volatile("s_nop 15\n\ts_nop 3" ::: "memory"); }
 __device__ __forceinline__ int lds_at(const void *p) { return (int)(uintptr_t)(__attribute__((address_space(3))) const void *)p; }
@@ -407,6 +408,7 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(2, 2)))
                 bf16x8_t kf[AHEAD];
 #pragma unroll
                 for (int ks = 0; ks < AHEAD; ++ks) kf[ks] = key_of(ks);
+                asm volatile("s_nop 1" : "+v"(n[0]), "+v"(n[1]));          // (two wait states from a vector instruction to a product that reads its result)
                 __builtin_amdgcn_s_setprio(1);
 #pragma unroll
                 for (int ks = 0; ks < C::KS; ++ks) {

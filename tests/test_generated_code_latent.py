@@ -101,3 +101,35 @@ def test_products_are_done_before_vector_instructions_touch_them(listings):
                 for r in _vectors(operands.split(",")[0]):
                     written.pop(r, None)
         assert products >= 16 + 36 or "Li256ELi32" in name and products >= 16 + 18, (name, products)
+
+
+def test_vector_instructions_are_done_before_products_read_them(listings):
+    """Two wait states between a vector instruction's result and a matrix instruction that reads it, on the way through the code in its
+    order and from every branch back to its target (results of loads are waited for by the compiler)."""
+    for name, body in _sweeps(listings[0]).items():
+        labels = {l[:-1]: i for i, l in enumerate(body) if l.endswith(":")}
+        ways = [range(len(body))]
+        for i, l in enumerate(body):
+            m = re.match(r"s_c?branch\w*\s+(\.L\w+)", l)
+            if m and m.group(1) in labels:
+                at = labels[m.group(1)]
+                ways.append([*range(max(0, i - 4), i + 1), *range(at, min(at + 4, len(body)))])
+        for way in ways:
+            states, written = 0, {}
+            for i in way:
+                l = body[i]
+                if l.startswith(".") or l.endswith(":"):
+                    continue
+                if l.startswith("s_nop"):
+                    states += int(l.split()[1], 0) + 1
+                    continue
+                operands = l.split(None, 1)[1] if len(l.split(None, 1)) > 1 else ""
+                if l.startswith("v_mfma"):
+                    close = [r for r in _vectors(operands) if r in written and states - written[r] < 2]
+                    assert not close, (name, l, close)
+                states += 1
+                if l.startswith("v_mfma"):
+                    for r in _vectors(operands.split(",")[0]):
+                        written.pop(r, None)
+                elif l.startswith("v_"):
+                    written.update((r, states) for r in _vectors(operands.split(",")[0]))
