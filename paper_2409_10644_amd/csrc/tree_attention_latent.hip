@@ -335,23 +335,51 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(2, 2)))
         const int slot = aligned ? 2 * w : 2 * w + (begun ? 1 : 0);
 
         if (scorer) {
-            // Query operands: rows col + 16 rg of this half of the chunk (behind the last: that one), channels 32 ks + 8 grp .. + 7.  And which
-            // tree nodes the rows see among this lane's 4 keys: 4 bits per row and tree tile.
+            // Query operands: rows col + 16 rg of this half of the chunk (behind the last: that one), channels 32 ks + 8 grp .. + 7.  They come by
+            // way of the places of tiles 2 and 3, whole cache lines, once for both wavefronts that
+            // share them (each by itself, 16 rows an instruction and half a line of each, waited 11500 cycles for them: 16 heads under 14 nodes and 128
+            // keys 18.5 us instead of 15.9, 16 x 512..4096 keys under 60 nodes 115 instead of 108).
+            // And which tree nodes the rows see among this lane's 4 keys: 4 bits per row and tree tile.
             bf16x8_t q[2][C::KS];
             uint64_t bits[2][2];
-            const uint16_t *src[2];
+            unsigned char *const queries = lds + 2 * C::TILE;
+            auto query_row = [&](int row, int &i) __attribute__((always_inline)) {                 // of the chunk: its place, its node
+                const int r = min(chunk * ROWS + row, p.rows - 1), h = row_div(r, p.by_nrows);
+                i = p.row0 + r - h * (p.n - p.row0);
+                return (const unsigned char *)(p.q + (((int64_t)b * p.H + h) * p.node_stride + i) * C::D);
+            };
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {                         // 8 rows of a panel per instruction
+                const int row = 16 * wave + 8 * half + (lane >> 3);
+                int i;
+                const unsigned char *src = query_row(row, i) + (((lane & 7) ^ swz(row & 15)) << 4);
+#pragma unroll
+                for (int x = 0; x < C::PANELS + (DR == 64); ++x) load_to_lds16_at(src + x * 128, queries + x * 2 * C::PANEL + (16 * wave + 8 * half) * 128);
+            }
+            if constexpr (DR == 32) {
+                const int row = 16 * wave + (lane >> 2);
+                int i;
+                const unsigned char *src = query_row(row, i) + C::PANELS * 128 + (((lane & 3) ^ swz_half(row & 15)) << 4);
+                load_to_lds16_at(src, queries + C::PANELS * 2 * C::PANEL + 16 * wave * 64);
+            }
 #pragma unroll
             for (int rg = 0; rg < 2; ++rg) {
-                const int r = min(chunk * ROWS + 32 * rh + 16 * rg + col, p.rows - 1), h = row_div(r, p.by_nrows), i = p.row0 + r - h * (p.n - p.row0);
-                src[rg] = p.q + (((int64_t)b * p.H + h) * p.node_stride + i) * C::D + 8 * grp;
+                int i;
+                query_row(32 * rh + 16 * rg + col, i);
                 const uint64_t *row = p.mask_bits + (int64_t)i * p.mask_words;
                 bits[rg][0] = row[0];
                 bits[rg][1] = tree_tiles > 2 ? row[1] : 0;
             }
+            MCSD_WAIT_VMCNT(0);
+            meet();                                                        // the queries are here
 #pragma unroll
             for (int rg = 0; rg < 2; ++rg)
 #pragma unroll
-                for (int ks = 0; ks < C::KS; ++ks) q[rg][ks] = *(const bf16x8_t *)(src[rg] + 32 * ks);
+                for (int ks = 0; ks < C::KS; ++ks) {
+                    const int row = 32 * rh + 16 * rg + col;
+                    q[rg][ks] = *(const bf16x8_t *)(queries + (DR == 32 && ks == C::KS - 1 ? C::PANELS * 2 * C::PANEL + row * 64 + ((grp ^ swz_half(col)) << 4)
+                                                                                            : (ks >> 1) * 2 * C::PANEL + row * 128 + (((grp + 4 * (ks & 1)) ^ swz(col)) << 4)));
+                }
             unsigned seen = 0;
 #pragma unroll
             for (int k = 0; k < 8; ++k) seen |= (unsigned)((bits[k & 1][k >> 2] >> (32 * (k >> 1 & 1) + 16 * kg + 4 * grp)) & 15) << (4 * k);      // tile k / 2, rows k % 2
@@ -501,6 +529,7 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(2, 2)))
                 for (int cb = 0; cb < C::CB; ++cb) o[rg][cb] = (f32x4_t){0, 0, 0, 0};
             request(0);
             if (count > 1) request(1);
+            meet();                                                        // the queries are here
             if (count > 1) MCSD_WAIT_VMCNT(C::LOADS);
             else MCSD_WAIT_VMCNT(0);
             meet();                                                        // the first tile is here
