@@ -219,20 +219,21 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(2, 2)))
             base_l = p.seq_base[b0 + lane];
         }
     };
-    fetch(0);
+    const bool uncut = !p.header;                                          // one workgroup for every unit: nothing to plan
+    if (!uncut) fetch(0);
     auto tiles_at = [&](int b0) __attribute__((always_inline)) {           // of sequence b0 + lane
         if (b0 != b_lanes) fetch(b0);
         return len_l >= 0 ? tree_tiles + (int)(((unsigned)len_l + KEYS - 1) / KEYS) : 0;
     };
     int total = 0, most = 0;
-    for (int b0 = 0; b0 < p.B; b0 += 64) {
+    for (int b0 = 0; b0 < p.B && !uncut; b0 += 64) {
         const int t = tiles_at(b0);
         total += wave_last(wave_scan(t));
         most = max(most, wave_max(t));
     }
     const int pairs = p.B * p.chunks, least = max(MIN_TILES, (int)(0.5f * __builtin_amdgcn_sqrtf((float)most)));
     int per = max((int)(((int64_t)total * p.chunks + G - 1) / G), least), aligned = 0;
-    if (pairs <= G) {
+    if (pairs <= G && !uncut) {
         if (per >= most) {
             aligned = per;
         } else {
@@ -257,14 +258,20 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(2, 2)))
     // leave too many workgroups without work, each at a place of its own: the ragged batch of 16 sequences of 512 to 4096 keys, 15 chunks
     // each, took 150 us, at 7 TB/s from behind the L2.)
     bool in_step = false;
-    if (!aligned && p.chunks <= G) {
+    if (!aligned && !uncut && p.chunks <= G) {
         const int teams = G / p.chunks, of_team = max((total + teams - 1) / teams, least);
         in_step = (int64_t)of_team * 4 <= (int64_t)per * 5;
         if (in_step) per = of_team;
     }
     // b, chunk: where the piece begins; tile: its first tile there; left: its tiles in all
     int b = -1, chunk = 0, tile = 0, left = 0, n_pieces = 1, number = 0, each = 0;
-    if (aligned) {
+    if (uncut) {
+        b = small_div(w, p.chunks);
+        chunk = w - b * p.chunks;
+        left = 0x7fffffff;
+        aligned = 1;
+        fetch(b & ~63);
+    } else if (aligned) {
         int before = 0;
         for (int b0 = 0; b0 < p.B && b < 0; b0 += 64) {
             const int t = tiles_at(b0), e = small_div(t + aligned - 1, aligned), s = wave_scan(e * p.chunks);
@@ -303,7 +310,7 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(2, 2)))
         }
     }
     if (b < 0 || left <= 0) {
-        if (p.header && tid == 0 && pairs > G) p.header[w].pieces = 0;
+        if (tid == 0 && pairs > G) p.header[w].pieces = 0;
         return;
     }
 
@@ -705,7 +712,8 @@ __global__ __launch_bounds__(256) void tree_attn_latent_fold_kernel(const Latent
 // ---------------------------------------------------------------------------------------------------- host
 struct LatentPlan {
     int chunks, workgroups, slot_rows;
-    size_t bytes;                    // workspace; 0: no unit is ever cut
+    size_t bytes;                    // workspace; 0: no unit is ever cut.  (By the sizes alone, so that it serves smaller calls.)
+    bool cut;                        // whether units may be cut
 };
 
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
@@ -722,9 +730,21 @@ bool make_plan(int B, int H, int dl, int n_rows, int n, int max_prefix, LatentPl
     pl.workgroups = (int)(pieces < cus ? pieces : cus);
     pl.slot_rows = rows < ROWS ? (int)rows : ROWS;
     pl.bytes = 0;
-    if (pieces > pairs || pairs > cus) {
+    pl.cut = pieces > pairs || pairs > cus;
+    if (pl.cut) {
         const size_t slots = (size_t)2 * pl.workgroups, slot_rows = slots * pl.slot_rows;
         pl.bytes = WS_HEADER + WS_CTR_BYTES + align256(pl.workgroups * sizeof(LatentHeader)) + 2 * align256(slot_rows * 4) + slot_rows * dl * 4;
+    }
+    // Cutting the longest unit saves (tiles - tiles of a piece) turns of 0.94 us (0.69 with 256 channels) and costs the plan and a second
+    // launch, 4.5 us, and the parts' way out and back at 5.5 TB/s.  Two sequences x 128 heads x 14 nodes of 448 keys: whole 23.6 us, cut 26.2;
+    // 8 x 16 heads x 44 nodes of 256 keys (256 channels): 13.7, cut 20.2; 4 x 16 heads x 1 node of 320 keys: cut 15.2, whole 16.7.
+    if (pl.cut && pairs <= cus) {
+        const int64_t at_once = cus / pairs, wanted = (tiles + MIN_TILES - 1) / MIN_TILES, n_pieces = at_once < wanted ? at_once : wanted;
+        const double saved = (double)(tiles - (tiles + n_pieces - 1) / n_pieces) * (dl == 512 ? 0.94 : 0.69);
+        if (saved <= 4.5 + (double)(pairs * n_pieces) * pl.slot_rows * dl * 8 / 5.5e6) {
+            pl.cut = false;
+            pl.workgroups = (int)pairs;
+        }
     }
     return true;
 }
@@ -778,7 +798,7 @@ extern "C" int mcsd_tree_attention_latent(const mcsd_mask_view_t *mask, int32_t 
     p.workgroups = pl.workgroups; p.slot_rows = pl.slot_rows;
     p.by_nrows = row_div_of((uint32_t)(n - row_begin));
     p.c = softmax_scale * 1.4426950408889634f;
-    if (pl.bytes > 0) {
+    if (pl.cut) {
         char *ws = (char *)workspace + WS_HEADER + WS_CTR_BYTES;
         const size_t slot_rows = (size_t)2 * pl.workgroups * pl.slot_rows;
         p.header = (LatentHeader *)ws;
@@ -795,7 +815,7 @@ extern "C" int mcsd_tree_attention_latent(const mcsd_mask_view_t *mask, int32_t 
                                   : (pl.chunks == 1 ? tree_attn_latent_kernel<256, 32, true> : tree_attn_latent_kernel<256, 32, false>);
     mcsd_launch(MCSD_KERNEL_ATTN_SWEEP, kernel, dim3(pl.workgroups), dim3(THREADS), st, p);
     if (hipGetLastError() != hipSuccess) return MCSD_EHIP;
-    if (pl.bytes > 0) {
+    if (pl.cut) {
         auto fold = d_latent == 512 ? tree_attn_latent_fold_kernel<512> : tree_attn_latent_fold_kernel<256>;
         const int64_t units = (int64_t)B * pl.chunks;
         const unsigned headers = (unsigned)(units < pl.workgroups ? units : pl.workgroups), rows = 1024u / d_latent;
