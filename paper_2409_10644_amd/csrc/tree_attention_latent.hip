@@ -52,7 +52,7 @@ struct LatentParams {
 constexpr size_t WS_HEADER = 256, WS_CTR_BYTES = 64 * 1024;      // what other calls keep at the head of a workspace stays as it is
 constexpr float SLACK = 16.f;        // log2 of what a score may exceed the running reference by before the output is rescaled
 constexpr int ROWS = 64, KEYS = 32;  // query rows of a chunk, keys of a tile
-constexpr int MIN_TILES = 4, CROSS = 12;
+constexpr int MIN_TILES = 4, CROSS = 12, UNCUT = 16;
 constexpr int THREADS = 512;
 constexpr int GROWN = 1, WRONG = 2;  // of a tile: scores beyond a reference; scores of tree nodes, seen or not, that are not finite
 
@@ -605,36 +605,66 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(2, 2)))
                 meet();
                 if (t == count) break;
             }
-            // ---- the rows' output, or this part of it
+            // ---- the rows' output, or this part of it: 16 rows x 128 bytes at a time by way of LDS (where weights were), so that a store
+            // writes whole cache lines (8 bytes a lane from the registers, 32 a row, took 8200 cycles: 2 x 128 heads under 14 nodes and 192 keys 16.1 us
+            // instead of 14.9).
 #pragma unroll
             for (int rg = 0; rg < 4; ++rg) {
                 settle();
+                __builtin_amdgcn_sched_barrier(0);
+                if (chunk * ROWS + 16 * rg >= p.rows) break;
+                unsigned char *const own = lds + C::P_AT + part * 2048;
+                const int at = anew(lane), own_row = at >> 3, own_at = own_row * 128 + (((at & 7) ^ own_row) << 4);
 #pragma unroll
                 for (int cb = 0; cb < C::CB; ++cb) asm volatile("" : "+v"(o[rg][cb]));
-                const int row = 16 * rg + anew(col), r = chunk * ROWS + row;
+                const int c = at & 15, g = at >> 4, row = 16 * rg + c;
                 const float sum = *(const float *)(lds + C::MAX_AT + row * 4) + *(const float *)(lds + C::MAX_AT + (ROWS + row) * 4);
                 const float ref = *(const float *)(lds + C::ALPHA_AT + row * 4);
-                if (r < p.rows) {
+                unsigned char *dst[2];                                     // of rows own_row and own_row + 8
+                bool there[2];
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const int row = 16 * rg + 8 * half + own_row, r = chunk * ROWS + row;
+                    there[half] = r < p.rows;
                     if (whole) {
                         const int h = row_div(r, p.by_nrows), i = p.row0 + r - h * (p.n - p.row0);
-                        uint16_t *dst = p.out + (((int64_t)b * p.H + h) * p.node_stride + i) * DL + part * (DL / 4) + 4 * grp;
-                        const float inv = 1.f / sum;
-#pragma unroll
-                        for (int cb = 0; cb < C::CB; ++cb) {
-                            const f32x4_t x = o[rg][cb] * inv;
-                            const u32x2_t pk = {__builtin_bit_cast(unsigned, (bf16x2_t){(__bf16)x[0], (__bf16)x[1]}),
-                                                __builtin_bit_cast(unsigned, (bf16x2_t){(__bf16)x[2], (__bf16)x[3]})};
-                            *(u32x2_t *)(dst + 16 * cb) = pk;
-                        }
+                        dst[half] = (unsigned char *)(p.out + (((int64_t)b * p.H + h) * p.node_stride + i) * DL + part * (DL / 4) + (at & 7) * 8);
                     } else {
-                        const int64_t at = (int64_t)slot * p.slot_rows + row;
-                        if (part == 0 && grp == 0) {
-                            p.part_m[at] = ref;
-                            p.part_l[at] = sum;
-                        }
-                        float *dst = p.part_o + at * DL + part * (DL / 4) + 4 * grp;
+                        dst[half] = (unsigned char *)(p.part_o + ((int64_t)slot * p.slot_rows + row) * DL + part * (DL / 4) + (at & 7) * 4);
+                    }
+                }
+                auto store = [&](int x) __attribute__((always_inline)) {
 #pragma unroll
-                        for (int cb = 0; cb < C::CB; ++cb) *(f32x4_t *)(dst + 16 * cb) = o[rg][cb];
+                    for (int half = 0; half < 2; ++half) {
+                        const u32x4_t v = *(const u32x4_t *)(own + own_at + half * 1024);
+                        if (there[half]) *(u32x4_t *)(dst[half] + x * 128) = v;
+                    }
+                };
+                unsigned char *const to = own + c * 128;
+                if (whole) {
+                    const float inv = 1.f / sum;
+#pragma unroll
+                    for (int x = 0; x < C::CB / 4; ++x) {
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const f32x4_t y = o[rg][4 * x + k] * inv;
+                            const u32x2_t pk = {__builtin_bit_cast(unsigned, (bf16x2_t){(__bf16)y[0], (__bf16)y[1]}),
+                                                __builtin_bit_cast(unsigned, (bf16x2_t){(__bf16)y[2], (__bf16)y[3]})};
+                            *(u32x2_t *)(to + (((2 * k + (g >> 1)) ^ (c & 7)) << 4) + (g & 1) * 8) = pk;
+                        }
+                        store(x);
+                    }
+                } else {
+                    if (part == 0 && g == 0 && chunk * ROWS + row < p.rows) {
+                        const int64_t of = (int64_t)slot * p.slot_rows + row;
+                        p.part_m[of] = ref;
+                        p.part_l[of] = sum;
+                    }
+#pragma unroll
+                    for (int x = 0; x < C::CB / 2; ++x) {
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) *(f32x4_t *)(to + (((4 * k + g) ^ (c & 7)) << 4)) = o[rg][2 * x + k];
+                        store(x);
                     }
                 }
             }
@@ -737,8 +767,9 @@ bool make_plan(int B, int H, int dl, int n_rows, int n, int max_prefix, LatentPl
     }
     // Cutting the longest unit saves (tiles - tiles of a piece) turns of 0.94 us (0.69 with 256 channels) and costs the plan and a second
     // launch, 4.5 us, and the parts' way out and back at 5.5 TB/s.  Two sequences x 128 heads x 14 nodes of 448 keys: whole 23.6 us, cut 26.2;
-    // 8 x 16 heads x 44 nodes of 256 keys (256 channels): 13.7, cut 20.2; 4 x 16 heads x 1 node of 320 keys: cut 15.2, whole 16.7.
-    if (pl.cut && pairs <= cus) {
+    // 8 x 16 heads x 44 nodes of 256 keys (256 channels): 13.7, cut 20.2; 4 x 16 heads x 1 node of 320 keys: cut 15.2, whole 16.7.  Of sequences
+    // that differ, which the host does not know, more can be saved: of longer ones (16 x 512..4096 keys: 108 us, whole 134) all are planned.
+    if (pl.cut && pairs <= cus && tiles <= UNCUT) {
         const int64_t at_once = cus / pairs, wanted = (tiles + MIN_TILES - 1) / MIN_TILES, n_pieces = at_once < wanted ? at_once : wanted;
         const double saved = (double)(tiles - (tiles + n_pieces - 1) / n_pieces) * (dl == 512 ? 0.94 : 0.69);
         if (saved <= 4.5 + (double)(pairs * n_pieces) * pl.slot_rows * dl * 8 / 5.5e6) {
