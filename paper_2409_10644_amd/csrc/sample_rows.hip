@@ -12,9 +12,9 @@
 // so a border falls where 64 bits have it.  Probabilities are computed in fp32 pairs, or of a binary64 exponent.
 //
 // What bounds it, at 32000 logits a row: few rows, the passes and meetings of one workgroup one after the other (45 rows of bf16, top-k 50
-// with top-p and min-p: 21 us; 64 rows of fp32 with top-p and four distinct draws: 46 us; 32 rows of 131077, mixed: 135 us, the vector
+// with top-p and min-p: 21 us; 64 rows of fp32 with top-p and four distinct draws: 43 us; 32 rows of 131077, mixed: 125 us, the vector
 // instructions of the rows with a top-p alone, 7 in 10 cycles); many rows, the exponentials, made once for the sum and once for the row
-// (2816 rows of bf16: 185 us for 541 MB, 2.9 TB/s; kept between the two they would need the LDS that the second workgroup has).
+// (2816 rows of bf16: 166 us for 541 MB, 3.3 TB/s; kept between the two they would need the LDS that the second workgroup has).
 // Rows in LDS between the passes took 2 to 20 us longer, and so did requests two more turns ahead.
 #include <math.h>
 
@@ -54,6 +54,7 @@ struct Shared {
         };
         uint2 roll[HELD * THREADS];      // logit and index
     };
+    double table[64];                    // 2^(j / 64)
     u64 segment[MAX_SEGMENTS];           // sums of 512 tokens
     u64 wave[THREADS / 64];
     int32_t count[MAX_SEGMENTS];         // kept tokens of 512, then of all before them
@@ -73,25 +74,43 @@ __device__ __forceinline__ u64 place_of(float x, int i) { return (u64)ordered(x)
 
 __device__ __forceinline__ int index_of(u64 place) { return 0x3ffff - (int)(place & 0x3ffff); }
 
-// 2^y for y <= 0: the polynomial is 2^f on [-1/2, 1/2] interpolated at the 11 Chebyshev points, off by at most 2^-51.5 of it.
-__device__ __forceinline__ u64 weight_of(double y)
+// 2^(j / 64), rounded to nearest.
+__device__ const double powers_of_two[64] = {
+    0x1.0000000000000p+0, 0x1.02c9a3e778061p+0, 0x1.059b0d3158574p+0, 0x1.0874518759bc8p+0,
+    0x1.0b5586cf9890fp+0, 0x1.0e3ec32d3d1a2p+0, 0x1.11301d0125b51p+0, 0x1.1429aaea92de0p+0,
+    0x1.172b83c7d517bp+0, 0x1.1a35beb6fcb75p+0, 0x1.1d4873168b9aap+0, 0x1.2063b88628cd6p+0,
+    0x1.2387a6e756238p+0, 0x1.26b4565e27cddp+0, 0x1.29e9df51fdee1p+0, 0x1.2d285a6e4030bp+0,
+    0x1.306fe0a31b715p+0, 0x1.33c08b26416ffp+0, 0x1.371a7373aa9cbp+0, 0x1.3a7db34e59ff7p+0,
+    0x1.3dea64c123422p+0, 0x1.4160a21f72e2ap+0, 0x1.44e086061892dp+0, 0x1.486a2b5c13cd0p+0,
+    0x1.4bfdad5362a27p+0, 0x1.4f9b2769d2ca7p+0, 0x1.5342b569d4f82p+0, 0x1.56f4736b527dap+0,
+    0x1.5ab07dd485429p+0, 0x1.5e76f15ad2148p+0, 0x1.6247eb03a5585p+0, 0x1.6623882552225p+0,
+    0x1.6a09e667f3bcdp+0, 0x1.6dfb23c651a2fp+0, 0x1.71f75e8ec5f74p+0, 0x1.75feb564267c9p+0,
+    0x1.7a11473eb0187p+0, 0x1.7e2f336cf4e62p+0, 0x1.82589994cce13p+0, 0x1.868d99b4492edp+0,
+    0x1.8ace5422aa0dbp+0, 0x1.8f1ae99157736p+0, 0x1.93737b0cdc5e5p+0, 0x1.97d829fde4e50p+0,
+    0x1.9c49182a3f090p+0, 0x1.a0c667b5de565p+0, 0x1.a5503b23e255dp+0, 0x1.a9e6b5579fdbfp+0,
+    0x1.ae89f995ad3adp+0, 0x1.b33a2b84f15fbp+0, 0x1.b7f76f2fb5e47p+0, 0x1.bcc1e904bc1d2p+0,
+    0x1.c199bdd85529cp+0, 0x1.c67f12e57d14bp+0, 0x1.cb720dcef9069p+0, 0x1.d072d4a07897cp+0,
+    0x1.d5818dcfba487p+0, 0x1.da9e603db3285p+0, 0x1.dfc97337b9b5fp+0, 0x1.e502ee78b3ff6p+0,
+    0x1.ea4afa2a490dap+0, 0x1.efa1bee615a27p+0, 0x1.f50765b6e4540p+0, 0x1.fa7c1819e90d8p+0
+};
+
+// 2^y for y <= 0 as 2^(k / 64) 2^r with |r| <= 1/128: the first six terms of 2^r leave 2^-54 of it, in all it is off by at most 2^-51.5.
+// (A polynomial over [-1/2, 1/2] needs ten products where this one has five and a number from LDS: 32 rows of
+// 131077, mixed, 135 us instead of 127, 64 rows with top-p and four distinct draws 45.5 instead of 44.1.)
+__device__ __forceinline__ u64 weight_of(double y, const double *table)
 {
     y = fmax(y, -60.0);                                                    // (zero, without a branch)
-    const double shifted = y + 0x1.8p52, f = y - (shifted - 0x1.8p52);      // (the integer next to y: without the conversions, a quarter as fast)
-    const int n = (int)__builtin_bit_cast(u64, shifted);
-    double p = 0x1.e6063f7217bc6p-28;
-    p = fma(p, f, 0x1.b675bca4eeebbp-24);
-    p = fma(p, f, 0x1.62bfd47773353p-20);
-    p = fma(p, f, 0x1.ffcb54062e698p-17);
-    p = fma(p, f, 0x1.430913096fd9fp-13);
-    p = fma(p, f, 0x1.5d87fe9d7a584p-10);
-    p = fma(p, f, 0x1.3b2ab6fba1ddap-7);
-    p = fma(p, f, 0x1.c6b08d703ce49p-5);
-    p = fma(p, f, 0x1.ebfbdff82c598p-3);
-    p = fma(p, f, 0x1.62e42fefa3a19p-1);
-    p = fma(p, f, 1.0);
-    // (times 2^(n + 45), and 2^52 added: the sum's last place is 1)
-    const double s = fma(p, __builtin_bit_cast(double, (u64)(unsigned)(n + ONE + 1023) << 52), 0x1p52);
+    const double shifted = y + 0x1.8p46, r = y - (shifted - 0x1.8p46);      // (the multiple of 1/64 next to y: without the conversions, a quarter as fast)
+    const int k = (int)__builtin_bit_cast(u64, shifted);
+    double p = 0x1.5d87fe78a6731p-10;
+    p = fma(p, r, 0x1.3b2ab6fba4e77p-7);
+    p = fma(p, r, 0x1.c6b08d704a0c0p-5);
+    p = fma(p, r, 0x1.ebfbdff82c58fp-3);
+    p = fma(p, r, 0x1.62e42fefa39efp-1);
+    p = fma(p, r, 1.0);
+    // (times 2^(k / 64 + 45), and 2^52 added: the sum's last place is 1)
+    const u64 power = __builtin_bit_cast(u64, table[k & 63]) + ((u64)(unsigned)((k >> 6) + ONE) << 52);
+    const double s = fma(p, __builtin_bit_cast(double, power), 0x1p52);
     return __builtin_bit_cast(u64, s) & 0xfffffffffffffull;
 }
 
@@ -218,6 +237,7 @@ __global__ __launch_bounds__(THREADS, 4) void sample_rows_kernel(const SamplePar
         }
     };
 
+    if (tid < 64) sh.table[tid] = powers_of_two[tid];
     // ---- maximum (NaN where a logit is), and whether the row is a distribution
     const float T = p.s.temperature ? p.s.temperature[b] : 1.f, top_p = p.s.top_p ? p.s.top_p[b] : 1.f, min_p = p.s.min_p ? p.s.min_p[b] : 0.f;
     const int top_k = p.s.top_k ? p.s.top_k[b] : 0;
@@ -246,7 +266,7 @@ __global__ __launch_bounds__(THREADS, 4) void sample_rows_kernel(const SamplePar
     float cut_x = LOWEST;                                                  // of everything but minus infinity
     int cut_i = V;
     auto exponent = [&](float x) { return ((double)x - mxd) * c; };
-    auto weight = [&](float x) { return weight_of(((double)x - top) * c); };
+    auto weight = [&](float x) { return weight_of(((double)x - top) * c, sh.table); };
     auto kept = [&](float x, int i) __attribute__((always_inline)) { return x > cut_x || (x == cut_x && i <= cut_i); };
     // each, but for wavefronts without a token from this logit on
     auto max8 = [](const Eight<F32> &x) { return fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7]))); };
@@ -324,7 +344,9 @@ __global__ __launch_bounds__(THREADS, 4) void sample_rows_kernel(const SamplePar
         each_kept([&](int, int i, const Eight<F32> &x) __attribute__((always_inline)) {
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-                const u64 m = kept(x[k], i + k) ? measure(x[k]) : 0;
+                u64 m = measure(x[k]);
+                asm volatile("" : "+v"(m));                                // (no branch around it: 127 -> 125 us for the mixed rows of 131077)
+                m = kept(x[k], i + k) ? m : 0;
                 if (m) atomicAdd(&sh.hist[bin_of(x[k])], m);
                 if (k % 2) __builtin_amdgcn_sched_barrier(0);              // (not all eight at once: registers)
             }
@@ -486,7 +508,9 @@ __global__ __launch_bounds__(THREADS, 4) void sample_rows_kernel(const SamplePar
             u64 here = 0;
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-                here += kept(x[k], i + k) && !(drawn >> k & 1) ? weight(x[k]) : 0;
+                u64 m = weight(x[k]);
+                asm volatile("" : "+v"(m));
+                here += kept(x[k], i + k) && !(drawn >> k & 1) ? m : 0;
                 if (k % 2) __builtin_amdgcn_sched_barrier(0);
             }
             const u64 s = wave_sum(here);
