@@ -12,7 +12,7 @@
 // so a border falls where 64 bits have it.  Probabilities are computed in fp32 pairs, or of a binary64 exponent.
 //
 // What bounds it, at 32000 logits a row: few rows, the passes and meetings of one workgroup one after the other (45 rows of bf16, top-k 50
-// with top-p and min-p: 21 us; 64 rows of fp32 with top-p and four distinct draws: 43 us; 32 rows of 131077, mixed: 125 us, the vector
+// with top-p and min-p: 21 us; 64 rows of fp32 with top-p and four distinct draws: 39 us; 32 rows of 131077, mixed: 116 us, the vector
 // instructions of the rows with a top-p alone, 7 in 10 cycles); many rows, the exponentials, made once for the sum and once for the row
 // (2816 rows of bf16: 166 us for 541 MB, 3.3 TB/s; kept between the two they would need the LDS that the second workgroup has).
 // Rows in LDS between the passes took 2 to 20 us longer, and so did requests two more turns ahead.
@@ -171,6 +171,11 @@ struct __attribute__((aligned(16))) Eight {
         if constexpr (F32) return __uint_as_float(w[k]);
         else return __uint_as_float(k & 1 ? w[k / 2] & 0xffff0000u : w[k / 2] << 16);
     }
+    __device__ __forceinline__ void drop(int k)                            // minus infinity
+    {
+        if constexpr (F32) w[k] = 0xff800000u;
+        else w[k / 2] = k & 1 ? (w[k / 2] & 0xffffu) | 0xff800000u : (w[k / 2] & 0xffff0000u) | 0xff80u;
+    }
 };
 
 template <bool F32, int THREADS>
@@ -265,20 +270,38 @@ __global__ __launch_bounds__(THREADS, 4) void sample_rows_kernel(const SamplePar
     constexpr float LOWEST = -3.402823466e38f;
     float cut_x = LOWEST;                                                  // of everything but minus infinity
     int cut_i = V;
+    float below = -INFINITY;                                               // the next number below cut_x
     auto exponent = [&](float x) { return ((double)x - mxd) * c; };
     auto weight = [&](float x) { return weight_of(((double)x - top) * c, sh.table); };
     auto kept = [&](float x, int i) __attribute__((always_inline)) { return x > cut_x || (x == cut_x && i <= cut_i); };
-    // each, but for wavefronts without a token from this logit on
+    auto cut_at = [&](float x, int i) {
+        cut_x = x;
+        cut_i = i;
+        below = x == 0.f ? -0x1p-149f : of_ordered(ordered(x) - 1);
+    };
+    // Of the eight tokens from i on those are kept whose logit exceeds the number returned: which index of a tie at the cut is kept is the
+    // same for all eight, but for the eight it falls into (there it is dropped beforehand).  So every pass has one compare for a token, not
+    // three (64 rows with top-p and four distinct draws 43 us, 39 so; 32 rows of 131077, mixed, 125 and 116).
+    auto sift = [&](Eight<F32> &x, int i) __attribute__((always_inline)) {
+        if (i <= cut_i && i + 7 > cut_i) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (i + k > cut_i && x[k] == cut_x) x.drop(k);
+        }
+        return i <= cut_i ? below : cut_x;
+    };
+    // each, sifted, but for wavefronts without a token from this logit on
     auto max8 = [](const Eight<F32> &x) { return fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7]))); };
     auto each_kept = [&](auto f, float from) __attribute__((always_inline)) {
         each([&](int t, int i, const Eight<F32> &x) __attribute__((always_inline)) {
-            if (__builtin_amdgcn_ballot_w64(max8(x) >= from) != 0) f(t, i, x);
+            if (__builtin_amdgcn_ballot_w64(max8(x) >= from) != 0) {
+                Eight<F32> y = x;
+                const float limit = sift(y, i);
+                f(t, i, y, limit);
+            }
         });
     };
-    auto set_cut = [&](u64 place, bool whole) {
-        cut_x = of_ordered((unsigned)(place >> 18));
-        cut_i = whole ? V : index_of(place);
-    };
+    auto set_cut = [&](u64 place, bool whole) { cut_at(of_ordered((unsigned)(place >> 18)), whole ? V : index_of(place)); };
     auto clear = [&]() {
         sh.hist[tid] = 0;
         sh.hist[tid + THREADS] = 0;
@@ -341,12 +364,12 @@ __global__ __launch_bounds__(THREADS, 4) void sample_rows_kernel(const SamplePar
         const float range = 31.9f * T, scale = range < INFINITY ? (BINS - 0.5f) / range : 0.f;      // (weights are zero beyond it)
         auto bin_of = [&](float x) { return scale < INFINITY ? (int)fminf((mx - x) * scale, (float)(BINS - 1)) : 0; };
         clear();
-        each_kept([&](int, int i, const Eight<F32> &x) __attribute__((always_inline)) {
+        each_kept([&](int, int i, const Eight<F32> &x, float limit) __attribute__((always_inline)) {
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
                 u64 m = measure(x[k]);
                 asm volatile("" : "+v"(m));                                // (no branch around it: 127 -> 125 us for the mixed rows of 131077)
-                m = kept(x[k], i + k) ? m : 0;
+                m = x[k] > limit ? m : 0;
                 if (m) atomicAdd(&sh.hist[bin_of(x[k])], m);
                 if (k % 2) __builtin_amdgcn_sched_barrier(0);              // (not all eight at once: registers)
             }
@@ -354,10 +377,10 @@ __global__ __launch_bounds__(THREADS, 4) void sample_rows_kernel(const SamplePar
         choose(0, goal);
         const int bin = sh.bin;
         u64 above = sh.above, lo = 0, hi = ~0ull;
-        each_kept([&](int, int i, const Eight<F32> &x) __attribute__((always_inline)) {
+        each_kept([&](int, int i, const Eight<F32> &x, float limit) __attribute__((always_inline)) {
             unsigned wanted = 0;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) wanted |= bin_of(x[k]) == bin && kept(x[k], i + k) ? 1u << k : 0;
+            for (int k = 0; k < 8; ++k) wanted |= bin_of(x[k]) == bin && x[k] > limit ? 1u << k : 0;
             append(x, i, wanted);
         }, cut_x);
         __syncthreads();
@@ -438,7 +461,7 @@ __global__ __launch_bounds__(THREADS, 4) void sample_rows_kernel(const SamplePar
     };
     if (T == 0.f || top_k == 1) {                                          // the largest alone
         int first = V;
-        each_kept([&](int, int i, const Eight<F32> &x) __attribute__((always_inline)) {
+        each_kept([&](int, int i, const Eight<F32> &x, float limit) __attribute__((always_inline)) {
 #pragma unroll
             for (int k = 7; k >= 0; --k) first = x[k] == mx && i + k < first ? i + k : first;
         }, mx);
@@ -482,8 +505,7 @@ __global__ __launch_bounds__(THREADS, 4) void sample_rows_kernel(const SamplePar
                     else out = mid;
                 }
                 if (of_ordered(in) > cut_x) {
-                    cut_x = of_ordered(in);
-                    cut_i = V;
+                    cut_at(of_ordered(in), V);
                     exact = false;
                 }
             }
@@ -503,14 +525,14 @@ __global__ __launch_bounds__(THREADS, 4) void sample_rows_kernel(const SamplePar
         u64 part = 0;
         for (int s = tid; s < turns * WAVES; s += THREADS) sh.segment[s] = 0;
         __syncthreads();
-        each_kept([&](int t, int i, const Eight<F32> &x) __attribute__((always_inline)) {
+        each_kept([&](int t, int i, const Eight<F32> &x, float limit) __attribute__((always_inline)) {
             const unsigned drawn = drawn_of(i, without);
             u64 here = 0;
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
                 u64 m = weight(x[k]);
                 asm volatile("" : "+v"(m));
-                here += kept(x[k], i + k) && !(drawn >> k & 1) ? m : 0;
+                here += x[k] > limit && !(drawn >> k & 1) ? m : 0;
                 if (k % 2) __builtin_amdgcn_sched_barrier(0);
             }
             const u64 s = wave_sum(here);
@@ -554,9 +576,12 @@ __global__ __launch_bounds__(THREADS, 4) void sample_rows_kernel(const SamplePar
         each([&](int, int i, const Eight<F32> &x) __attribute__((always_inline)) {
             float e[8];
             powers(x, e);
-            if (!whole)
+            if (!whole) {
+                Eight<F32> z = x;
+                const float limit = sift(z, i);
 #pragma unroll
-                for (int k = 0; k < 8; ++k) e[k] = kept(x[k], i + k) ? e[k] : 0.f;
+                for (int k = 0; k < 8; ++k) e[k] = z[k] > limit ? e[k] : 0.f;
+            }
             part += (double)(((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7])));
         });
         // (in the order of the lanes and wavefronts: the same every time)
@@ -591,10 +616,10 @@ __global__ __launch_bounds__(THREADS, 4) void sample_rows_kernel(const SamplePar
         const int segments = turns * WAVES;
         for (int s = tid; s < segments; s += THREADS) sh.count[s] = 0;
         __syncthreads();
-        each_kept([&](int t, int i, const Eight<F32> &x) __attribute__((always_inline)) {
+        each_kept([&](int t, int i, const Eight<F32> &x, float limit) __attribute__((always_inline)) {
             int here = 0;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) here += kept(x[k], i + k);
+            for (int k = 0; k < 8; ++k) here += x[k] > limit;
             const int all = ::wave_last(::wave_scan(here));
             if (lane == 0) sh.count[t * WAVES + wave] = all;
         }, cut_x);
@@ -616,14 +641,14 @@ __global__ __launch_bounds__(THREADS, 4) void sample_rows_kernel(const SamplePar
         __syncthreads();
         if (sh.kept <= ROLL) {
             rolled = true;
-            each_kept([&](int t, int i, const Eight<F32> &x) __attribute__((always_inline)) {
+            each_kept([&](int t, int i, const Eight<F32> &x, float limit) __attribute__((always_inline)) {
                 int here = 0;
 #pragma unroll
-                for (int k = 0; k < 8; ++k) here += kept(x[k], i + k);
+                for (int k = 0; k < 8; ++k) here += x[k] > limit;
                 int at = sh.count[t * WAVES + wave] + ::wave_scan(here) - here;
 #pragma unroll
                 for (int k = 0; k < 8; ++k)
-                    if (kept(x[k], i + k)) sh.roll[at++] = make_uint2(__float_as_uint(x[k]), i + k);
+                    if (x[k] > limit) sh.roll[at++] = make_uint2(__float_as_uint(x[k]), i + k);
             }, cut_x);
             __syncthreads();
 #pragma unroll
@@ -649,9 +674,11 @@ __global__ __launch_bounds__(THREADS, 4) void sample_rows_kernel(const SamplePar
 #pragma unroll
                 for (int k = 0; k < 8; ++k) y[k] *= inv;
             } else if (__builtin_amdgcn_ballot_w64(max8(x) >= cut_x) != 0) {      // (the other wavefronts have zeros to write)
-                powers(x, y);
+                Eight<F32> z = x;
+                const float limit = sift(z, i);
+                powers(z, y);
 #pragma unroll
-                for (int k = 0; k < 8; ++k) y[k] = kept(x[k], i + k) ? y[k] * inv : 0.f;
+                for (int k = 0; k < 8; ++k) y[k] = z[k] > limit ? y[k] * inv : 0.f;
             }
             if (i < V) write8(i, y);
         });
@@ -779,12 +806,12 @@ __global__ __launch_bounds__(THREADS, 4) void sample_rows_kernel(const SamplePar
     for (int d = 0; d < p.n_draw; ++d) {
         if (d && sum < 1ull << FEW) {                                      // (the same for all threads)
             u64 best = 0;
-            each_kept([&](int, int i, const Eight<F32> &x) __attribute__((always_inline)) {
+            each_kept([&](int, int i, const Eight<F32> &x, float limit) __attribute__((always_inline)) {
                 const unsigned drawn = drawn_of(i, d);
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
                     const u64 at = place_of(x[k], i + k);
-                    if (at > best && kept(x[k], i + k) && !(drawn >> k & 1)) best = at;
+                    if (at > best && x[k] > limit && !(drawn >> k & 1)) best = at;
                 }
             }, cut_x);
             best = block_max(best);
