@@ -11,9 +11,6 @@
 // stands alone, 4500 cycles per 64 keys, of which the products are 2176.)
 #include <math.h>
 
-#include <atomic>
-#include <type_traits>
-
 #include "fp4_format.h"
 #include "wave_ops.h"
 
@@ -65,8 +62,6 @@ __device__ __forceinline__ const unsigned char *uniform(const unsigned char *a)
     return (const unsigned char *)((uint64_t)(uint32_t)uniform((int)(v >> 32)) << 32 | (uint32_t)uniform((int)v));
 }
 __device__ __forceinline__ void meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
-
-__device__ __forceinline__ void bare() { asm volatile("s_barrier" ::: "memory"); }
 __device__ __forceinline__ float max4(const f32x4_t &v)
 {
     float m;
