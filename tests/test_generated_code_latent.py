@@ -133,3 +133,29 @@ def test_vector_instructions_are_done_before_products_read_them(listings):
                         written.pop(r, None)
                 elif l.startswith("v_"):
                     written.update((r, states) for r in _vectors(operands.split(",")[0]))
+
+
+def test_the_variant_for_few_rows(listings):
+    """Both sizes are there, with as many products as their rows need, and its wait states are those of the others."""
+    few = {n: b for n, b in listings[0].items() if "tree_attn_latent_few_kernel" in n}
+    assert sorted(re.search(r"few_kernelILi(\d+)ELi(\d+)E", n).groups() for n in few) == [("256", "32"), ("512", "64")]
+    renamed = {n.replace("latent_few_kernel", "latent_kernel"): b for n, b in few.items()}
+    test_vector_instructions_are_done_before_products_read_them((renamed, {}))
+    for name, body in few.items():
+        products = [i for i, l in enumerate(body) if l.startswith("v_mfma")]
+        assert len(products) >= (18 + 8 if "Li512" in name else 9 + 4), name
+        for i in products:                                     # what a product writes, no other instruction touches within 11 wait states
+            written, states = _vectors(body[i].split(None, 1)[1].split(",")[0]), 0
+            for l in body[i + 1:]:
+                if l.startswith(".") or l.endswith(":"):
+                    continue
+                if l.startswith("s_nop"):
+                    states += int(l.split()[1], 0) + 1
+                    continue
+                if states >= 11 or l.startswith("s_cbranch") or l.startswith("s_branch"):
+                    break
+                operands = l.split(None, 1)[1] if len(l.split(None, 1)) > 1 else ""
+                if l.startswith("v_mfma"):
+                    operands = ", ".join(operands.split(", ")[1:3])
+                assert not written & _vectors(operands), (name, body[i], l)
+                states += 1

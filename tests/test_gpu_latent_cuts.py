@@ -26,3 +26,11 @@ def test_around_the_cut(binding, dl, dr, branching, H, lens):  # noqa: F811
 def test_more_sequences_than_lanes_stay_whole(binding):  # noqa: F811
     """A workgroup for every unit, the sequences' lengths read 64 at a time."""
     Call(binding, (2, 2), 16, 256, 32, tuple((37 * i) % 130 for i in range(130))).check()
+
+
+@pytest.mark.parametrize("dl,dr", SIZES)
+@pytest.mark.parametrize("branching,H", [((1,), 16), ((1,), 17), ((2, 2), 2), ((2, 2), 3), ((3, 1), 1), ((4, 2, 2), 1), ((8,), 2), ((17,), 1)])
+@pytest.mark.parametrize("lens,gain", [((0, 33, 700), 1.0), ((3000, 1), 8.0), ((95, 96, 97, 31), 30.0)])
+def test_around_16_rows(binding, dl, dr, branching, H, lens, gain):  # noqa: F811
+    """The variant for 16 rows and the other; large scores move the references."""
+    Call(binding, branching, H, dl, dr, lens, gain=gain).check()

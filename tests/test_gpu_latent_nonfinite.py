@@ -46,3 +46,10 @@ def test_all_nodes_but_one_branch(binding, dl, dr):  # noqa: F811
     torch.cuda.synchronize()
     assert torch.equal(c.out[0, :, :c.n][:, kept], want[0, :, :c.n][:, kept])
     assert bool(torch.isnan(c.out[0, :, :c.n][:, ~kept].float()).all())
+
+
+@pytest.mark.parametrize("branching,H,lens", [((2, 2), 2, (20, 300)), ((2, 1), 4, (2500,)), ((1, 1, 1), 5, (700, 0))])
+@pytest.mark.parametrize("dl,dr", SIZES)
+@pytest.mark.parametrize("value", [math.nan, math.inf, -math.inf])
+def test_no_more_than_16_rows(binding, branching, H, lens, dl, dr, value):  # noqa: F811
+    test_tree_rows_that_are_not_finite(binding, branching, H, lens, dl, dr, value)
