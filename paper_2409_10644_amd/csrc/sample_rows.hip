@@ -301,7 +301,12 @@ __global__ __launch_bounds__(THREADS, 4) void sample_rows_kernel(const SamplePar
             }
         });
     };
-    auto set_cut = [&](u64 place, bool whole) { cut_at(of_ordered((unsigned)(place >> 18)), whole ? V : index_of(place)); };
+    // The token at this place is the last that is kept; whole: all with its logit are, but for those that an earlier cut left out (a search
+    // sees the kept tokens only, so it cannot tell).
+    auto set_cut = [&](u64 place, bool whole) {
+        const float x = of_ordered((unsigned)(place >> 18));
+        cut_at(x, !whole ? index_of(place) : x == cut_x ? cut_i : V);
+    };
     auto clear = [&]() {
         sh.hist[tid] = 0;
         sh.hist[tid + THREADS] = 0;
