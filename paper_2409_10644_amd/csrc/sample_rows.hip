@@ -114,6 +114,11 @@ __device__ __forceinline__ u64 weight_of(double y, const double *table)
     return __builtin_bit_cast(u64, s) & 0xfffffffffffffull;
 }
 
+// A share in parts of 2^-64, kept within [0, 1) (NaN: 0): its product with a sum of weights is one of whole numbers.  (The sum of many
+// weights has more than the 53 bits of a binary64; a product rounded to those can be hundreds of the weights' last places off.  Shares below
+// 2^-40 lose their last bits here, half a last place of the product at most.)
+__device__ __forceinline__ u64 parts_of(float share) { return (u64)((double)fminf(fmaxf(share, 0.f), 0x1.fffffep-1f) * 0x1p64); }
+
 // From other lanes of the wavefront, zero where there is none (see wave_ops.h for the steps).
 template <int CTRL, int ROWS>
 __device__ __forceinline__ u64 from_lane64(u64 v)
@@ -445,7 +450,10 @@ __global__ __launch_bounds__(THREADS, 4) void sample_rows_kernel(const SamplePar
         set_cut(place, !__syncthreads_or(parted || (mine && mine >> 18 == place >> 18 && mine < place)));
         return sh.sum;
     };
-    auto share = [&](u64 all) { const double g = ceil((double)top_p * (double)all); return g < 1.0 ? (u64)1 : (u64)g; };      // of the sum, to top-p
+    auto share = [&](u64 all) {                                            // of the sum, to top-p: rounded up, 1 at least
+        const u64 goal = (u64)(((unsigned __int128)parts_of(top_p) * all + ~0ull) >> 64);
+        return goal ? goal : (u64)1;
+    };
 
     // Of the n listed tokens, all from the first on down to somewhere behind what is kept: what top-k, top-p and min-p leave.
     u64 sum = 0;
@@ -691,11 +699,7 @@ __global__ __launch_bounds__(THREADS, 4) void sample_rows_kernel(const SamplePar
     if (!p.n_draw) return;
 
     // ---- draws: the first token, in the order of indices, at which the sum of the weights exceeds u times all of it
-    auto goal_of = [&](float u) {
-        u = fminf(fmaxf(u, 0.f), 0x1.fffffep-1f);
-        const u64 goal = (u64)((double)u * (double)sum);
-        return goal < sum ? goal : sum - 1;
-    };
+    auto goal_of = [&](float u) { return __umul64hi(parts_of(u), sum); };   // (rounded down: below the sum)
     if (rolled) {
         // the thread that has it: which of its tokens
         auto take = [&](u64 goal) {
