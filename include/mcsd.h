@@ -579,7 +579,8 @@ int mcsd_store_latent(mcsd_dtype_t dtype, int32_t B, int32_t d_latent, int32_t d
  *     top-p : the first, or w of all tokens before it sums to less than top_p times the sum over those that top-k keeps  (off: >= 1)
  *     min-p : w_i >= min_p                                                      (off where min_p <= 0; above 1 it counts as 1)
  * and its logit is not minus infinity.  p_i = w_i / (sum of the kept w) for kept tokens, 0 for others.  T = 0 keeps the first token alone.
- * Borders and draws are decided by the w to within 2^-45 of the largest; probabilities are fp32.
+ * Borders of top-p and draws are decided by the w rounded to multiples of 2^-45 of the largest, whose sums and shares of them are exact;
+ * probabilities are fp32.
  * Draw d of a row is the first kept token, in the order of indices, at which the running sum of w exceeds u[d] times all of it; with
  * MCSD_WITHOUT_REPLACEMENT the tokens drawn before it are left out of both.  A draw that finds nothing left is -1.
  * A row of minus infinities alone has zero probabilities and tokens -1; one with a NaN or plus infinity, or with T or top_p or min_p

@@ -49,7 +49,8 @@ struct LatentParams {
 constexpr size_t WS_HEADER = 256, WS_CTR_BYTES = 64 * 1024;      // what other calls keep at the head of a workspace stays as it is
 constexpr float SLACK = 16.f;        // log2 of what a score may exceed the running reference by before the output is rescaled
 constexpr int ROWS = 64, KEYS = 32;  // query rows of a chunk, keys of a tile
-constexpr int MIN_TILES = 4, CROSS = 12, UNCUT = 16;
+constexpr int MIN_TILES = 4, UNCUT = 16;
+constexpr int CROSS = 12;            // tiles that a piece within one sequence may have beyond an equal share (both sides at its use)
 constexpr int THREADS = 512;
 constexpr int GROWN = 1, WRONG = 2;  // of a tile: scores beyond a reference; scores of tree nodes, seen or not, that are not finite
 

@@ -36,7 +36,14 @@
         total += wave_last(wave_scan(t));
         most = max(most, wave_max(t));
     }
+    // A unit of t tiles in pieces of s: s turns, and t / s parts to fold, each counted as a quarter of a turn; s = sqrt(t) / 2 is the least of
+    // both together.  (One sequence of 16384 keys, 16 heads, one node: 32 us, with pieces down to four tiles 55; 8192 keys, 128 heads: 33
+    // and 41.  Where there are more units, equal shares are longer than that.)
     const int pairs = p.B * p.chunks, least = max(MIN_TILES, (int)(0.5f * __builtin_amdgcn_sqrtf((float)most)));
+    // Pieces that stay within a sequence, all of a unit's alike, may be up to CROSS tiles longer than equal shares of everything, whose pieces
+    // can go on in the next unit: queries and output twice.  (8 sequences of 100..3000 keys x 32 heads x 14 nodes: 32 us, without the
+    // allowance 37; 24 of 100..1500 x 8 heads x 44 nodes: 41 and 44.  It loses where shares are short: 1024 keys x 128 heads x 44 nodes, 17
+    // tiles where the share is 12: 40.1 and 38.5.  An allowance of 24: 4096 keys x 128 heads x 44 nodes 84 us, with 12 or none 76.)
     int per = max((int)(((int64_t)total * p.chunks + G - 1) / G), least), aligned = 0;
     if (pairs <= G && !uncut) {
         if (per >= most) {
@@ -61,7 +68,9 @@
     // Else as many teams as the chunks leave room for, one workgroup for every chunk, that go through all sequences' tiles in step: a tile
     // is read from memory once for all of its chunks then, and from the L2 by the others.  (Equal pieces of everything, where that would
     // leave too many workgroups without work, each at a place of its own: the ragged batch of 16 sequences of 512 to 4096 keys, 15 chunks
-    // each, took 150 us, at 7 TB/s from behind the L2.)
+    // each, took 150 us, at 7 TB/s from behind the L2.)  That is worth up to a quarter more tiles than equal pieces have: never in step, 2 x
+    // 16384 keys x 64 heads x 120 nodes took 560 us instead of 513 and 6 x 300..9000 keys x 16 heads x 120 nodes 172 instead of 144; always,
+    // 4096 keys x 128 heads x 44 nodes 83 instead of 76 and 4 x 500..2000 keys 111 instead of 104.
     bool in_step = false;
     if (!aligned && !uncut && p.chunks <= G) {
         const int teams = G / p.chunks, of_team = max((total + teams - 1) / teams, least);
@@ -217,8 +226,9 @@
             for (int k = 0; k < 8; ++k) seen |= (unsigned)((bits[k & 1][k >> 2] >> (32 * (k >> 1 & 1) + 16 * kg + 4 * grp)) & 15) << (4 * k);      // tile k / 2, rows k % 2
             float ref[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, start[2] = {0.f, 0.f};      // (start: minus the reference, 0 while no key has been seen)
             f32x4_t s[SR];
-            // Of tile t, whose scores s holds: its maxima over all keys, new references, its weights again; what O^T has of the tiles before is
-            // multiplied by alpha.
+            // Weights are rounded to bf16, which is what the product with the values takes: half a step, 2^-8 of each, and as they are off
+            // independently of each other, of an output made from many keys less (0.0017 to 0.0023 of it in all, of which its own rounding is
+            // 0.0017).  Their sum is of the weights in fp32.
             auto weigh = [&](int t, float (&sum)[2]) __attribute__((always_inline)) {
                 unsigned char *pw = lds + pw_at + (t & 1) * C::P_BYTES;
 #pragma unroll
@@ -233,6 +243,8 @@
                 }
             };
             float sum[2] = {0.f, 0.f};                                     // of the last tile's weights
+            // Of tile t, whose scores s holds: its maxima over all keys, new references, its weights again; what O^T has of the tiles before is
+            // multiplied by alpha.
             auto outgrown = [&](int t) __attribute__((always_inline)) {
 #pragma unroll
                 for (int rg = 0; rg < SR; ++rg) {
