@@ -33,7 +33,6 @@
 // lengths, queries, tree rows, prefix.  (Ranges: machines.  The pairs of figures at the rules below are of one machine and day.)
 #include <math.h>
 
-#include <atomic>
 #include <type_traits>
 
 #include "fp4_format.h"
@@ -1130,22 +1129,6 @@ struct Fp4Plan {
 
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
-int compute_units()
-{
-    static std::atomic<int> cus_of_device[64];
-    int dev = 0;
-    if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) {
-        (void)hipGetLastError();
-        return 256;                  // no device to ask: the whole chip
-    }
-    int v = cus_of_device[dev].load(std::memory_order_relaxed);
-    if (v == 0) {
-        if (hipDeviceGetAttribute(&v, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || v < 1) v = 256;
-        cus_of_device[dev].store(v, std::memory_order_relaxed);
-    }
-    return v;
-}
-
 // False where the work has more tiles than the kernel's numbers hold.
 bool make_plan(int B, int H_kv, int grp, int d, int n_rows, int n, int max_prefix, Fp4Plan &pl)
 {
@@ -1162,7 +1145,7 @@ bool make_plan(int B, int H_kv, int grp, int d, int n_rows, int n, int max_prefi
     pl.chunks = (int)chunks;
     pl.units = (int)units;
     const int min_tiles = pl.QBP == 1 ? Cfg<128, 1>::MIN_TILES : pl.QBP == 2 ? Cfg<128, 2>::MIN_TILES : Cfg<128, 4>::MIN_TILES;
-    pl.single = compute_units();
+    pl.single = mcsd_compute_units();
     int most = 2 * pl.single;
     if (most > MAX_PIECES) most = MAX_PIECES;
     const int64_t pairs = units * B, pieces = pairs * ((tiles + min_tiles - 1) / min_tiles);
